@@ -3,7 +3,7 @@
  * hot path (arXiv 2412.11741, "CSR: Achieving 1 Bit Key-Value Cache via Sparse
  * Representation").
  *
- * Two operations:
+ * The two operations of the method (restore, Gram matrices and checks beside them; a 4-bit cache to compare with below):
  *   csr_encode       greedy Matching Pursuit of dense per-head key/value vectors into s
  *                    (atom index, coefficient) pairs against a per-head dictionary
  *                    (Section "Sparse representation", Eq.2-4; Section "KV Decomposition and
@@ -48,7 +48,11 @@ typedef enum {
     CSR_ERR_DEVICE = 4       /* the HIP runtime reported an error while enqueuing          */
 } csr_status;
 
-typedef enum { CSR_F32 = 0, CSR_F16 = 1 } csr_dtype; /* vectors, dictionaries, coefficients */
+typedef enum {
+    CSR_F32 = 0,
+    CSR_F16 = 1, /* vectors, dictionaries, coefficients */
+    CSR_BF16 = 2 /* the csr_q4 calls' dense vectors, queries and outputs only */
+} csr_dtype;
 typedef enum { CSR_I32 = 0, CSR_I16 = 1 } csr_itype; /* atom indices; I16 is unsigned        */
 
 /* Which encoder kernel runs.  AUTO picks SPLIT when a dictionary serves few vectors (the tokens of one
@@ -307,6 +311,110 @@ csr_status csr_atom_norms2(const void *D, int32_t dict_dtype, int64_t n_atoms, i
  *   bad    device, one int64, 8-byte aligned                     out (valid once the stream has run)
  */
 csr_status csr_check_codes(const void *idx, int32_t idx_dtype, int64_t count, int32_t N, int64_t *bad, void *hip_stream);
+
+/*
+ * ---- A cache held in 4 bits -------------------------------------------------------------------------------------------
+ * The dense alternative to the codes above: keys and values as 4-bit numbers with a scale and a minimum per group of
+ * channels of every token (the group-wise integer caches that Tables 1 and 2 compare with).  Written as tokens arrive
+ * (csr_q4_write), read back (csr_q4_read), attended over (csr_q4_attn).
+ *
+ *   codes  [B][Hkv][T][d/2]       uint8: byte j holds channel 2j in its low half, channel 2j+1 in its high half
+ *   params [B][Hkv][d/group][T][2] fp16: scale s and minimum m of channels k*group .. (k+1)*group - 1 of the token
+ *   value  = fp16(s * code + m), rounded once - for csr_q4_read and csr_q4_attn alike
+ *
+ * With x' the group's values held to +-65504:  m = fp16(min x'), s = (max x' - m)/15 rounded to fp16 toward zero (at
+ * least 0), code = (x' - m)/s rounded to the nearest whole number, halves to even, held to 0..15 (0 where s = 0).  All
+ * of it is as exact arithmetic gives it.  A value never reads back as an infinity.  A group that holds a NaN or an
+ * infinity gets s = m = NaN: it reads back as NaN, and attention that sees the token gives NaN in those channels (a
+ * value) or everywhere (a key).
+ *
+ * Both arrays are contiguous, codes 16-byte and params 4-byte aligned; a row no call has written holds whatever was there.
+ */
+typedef struct {
+    int32_t B;          /* sequences; >= 0                                                  */
+    int32_t Hkv;        /* KV heads                                                         */
+    int64_t n;          /* rows of X / out per (b, h); >= 0                                 */
+    int64_t T;          /* rows allocated per (b, h) in the cache; 0 .. 2^20                */
+    int32_t d;          /* head dimension: 64 or 128                                        */
+    int32_t group;      /* channels per scale: 32, 64 or 128, at most d                     */
+    int32_t x_dtype;    /* csr_dtype of X (csr_q4_read: ignored, its strides too)                         */
+    int64_t x_stride_b, x_stride_h, x_stride_t;       /* elements between sequences, heads, tokens of X, as they
+                           are (no defaults); multiples of 16 bytes, >= 0                   */
+    int32_t out_dtype;  /* csr_dtype of out                                                 */
+    int64_t out_stride_b, out_stride_h, out_stride_t; /* likewise for out; >= d where there is more than one       */
+    int64_t pos0;       /* row t of X / out is row pos0 + pos[b] + t of the cache; |pos0| <= 2^40                   */
+    uint32_t flags;     /* must be 0                                                        */
+} csr_q4_rows_desc;
+
+/* Bytes kept per head vector: d/2 + 4 * (d/group).  Returns 0 on bad arguments. */
+size_t csr_q4_bytes(int32_t d, int32_t group);
+
+/*
+ * Quantise rows of X into the cache; a second tensor (the values beside the keys) in the same launch.
+ *   X       [B][Hkv][n][d]  (strides as given), 16-byte aligned     in
+ *   codes, params           the cache                               out: rows written as above, the others untouched
+ *   out     [B][Hkv][n][d]  or NULL, 16-byte aligned                out: the values that the cache now stands for
+ *   pos     [B] int32 device pointer, or NULL for 0: added to pos0
+ *   counts  [B] int32 device pointer, or NULL for n: rows of every sequence that hold a token (a padded batch)
+ * Rows t >= counts[b], and rows that fall outside 0 .. T-1, are written nowhere; in out they are zeros.
+ * desc2 (with X2, codes2, params2, out2) may be NULL.  It must agree with desc in B, Hkv, n, T, d, x_dtype, out_dtype and
+ * pos0; group and strides are its own.  out and out2 are both given or both NULL.  No workspace.
+ */
+csr_status csr_q4_write(const csr_q4_rows_desc *desc, const void *X, void *codes, void *params, void *out,
+                        const csr_q4_rows_desc *desc2, const void *X2, void *codes2, void *params2, void *out2,
+                        const int32_t *pos, const int32_t *counts, void *hip_stream);
+
+/*
+ * out[b][h][t] = the values of cache row pos0 + pos[b] + t, for t < counts[b] and rows inside the cache; zeros elsewhere.
+ * pos and counts as above.  No workspace.
+ */
+csr_status csr_q4_read(const csr_q4_rows_desc *desc, const void *codes, const void *params, void *out, const int32_t *pos,
+                       const int32_t *counts, void *hip_stream);
+
+/*
+ * Softmax attention of Tq query tokens per sequence over the cache.  The queries are the sequence's last tokens: with
+ * qn = q_lens[b] (Tq without q_lens), query i < qn stands at token len_b - qn + i and sees the tokens up to it - its own
+ * key is in the cache already.  With CSR_FLAG_NOT_CAUSAL every query sees all len_b tokens.  Queries i >= qn, and those
+ * that see no token, yield zeros.  What the cache holds behind a sequence's last token, or behind the tokens a query
+ * sees, never reaches its output, NaN included.  Products of values and probabilities, scores and sums are fp32; the
+ * query enters as fp16 (fp16 as it is, bf16 and
+ * fp32 times a power of two per head vector, bf16 without loss down to 2^-28 of the vector's largest, fp32 as two fp16),
+ * probabilities as one fp16 (more than 64 query rows per KV head, fp16 and bf16 queries) or two.  The same inputs give
+ * the same bits on every run.
+ */
+#define CSR_FLAG_NOT_CAUSAL 1u
+typedef struct {
+    int32_t B;          /* sequences; >= 0                                                  */
+    int32_t Hq;         /* query heads; multiple of Hkv                                     */
+    int32_t Hkv;        /* KV heads                                                         */
+    int32_t Tq;         /* query tokens per sequence; >= 0                                  */
+    int64_t T;          /* rows allocated per (b, h) in the cache; 0 .. 2^20                */
+    int32_t d;          /* head dimension: 64 or 128                                        */
+    int32_t group_k, group_v; /* channels per scale of keys and of values: 32, 64 or 128, at most d          */
+    float scale;        /* score scale; 0 means 1/sqrt(d)                                   */
+    int32_t q_dtype;    /* csr_dtype of q                                                   */
+    int32_t out_dtype;  /* csr_dtype of out                                                 */
+    int64_t q_stride_b, q_stride_h, q_stride_t;       /* elements between sequences, heads, tokens of q, as they
+                           are (no defaults); multiples of 16 bytes, >= 0                   */
+    int64_t out_stride_b, out_stride_h, out_stride_t; /* likewise for out; >= d where there is more than one       */
+    uint32_t flags;     /* CSR_FLAG_NOT_CAUSAL or 0                                         */
+} csr_q4_attn_desc;
+
+/* Bytes of device scratch csr_q4_attn needs (may be 0); (size_t)-1 if the descriptor is invalid. */
+size_t csr_q4_attn_workspace_bytes(const csr_q4_attn_desc *desc);
+
+/*
+ *   q        [B][Hq][Tq][d]  (strides as given), 16-byte aligned   in
+ *   codesK, paramsK, codesV, paramsV                               in, the caches of keys and of values
+ *   seq_lens [B] int32 device pointer, or NULL for len_b = T; larger values count as T, negative ones as 0
+ *   q_lens   [B] int32 device pointer, or NULL for Tq; held to 0 .. Tq
+ *   out      [B][Hq][Tq][d]  (strides as given), 16-byte aligned   out
+ *   workspace: device memory, 256-byte aligned, >= csr_q4_attn_workspace_bytes(); may be NULL when that is 0.  Contents
+ *   are undefined before and after; calls that may overlap need one each.
+ */
+csr_status csr_q4_attn(const csr_q4_attn_desc *desc, const void *q, const void *codesK, const void *paramsK,
+                       const void *codesV, const void *paramsV, const int32_t *seq_lens, const int32_t *q_lens, void *out,
+                       void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /*
  * Storage accounting of Section "Analysis for CSR": bytes kept per head vector,

@@ -4,7 +4,7 @@ Argument marshalling only: every step of the hot path runs in the HIP kernels.  
 used for device memory and the current stream.  There is no CPU fallback: if the library is
 missing, or a tensor is not on the GPU, the call raises.
 
-csr_encode, csr_decode_attn and csr_reconstruct first hand their arguments to the compiled marshalling of
+csr_encode, csr_decode_attn, csr_reconstruct and the csr_q4 calls first hand their arguments to the compiled marshalling of
 csrc/torch_binding (1 - 2 us of host time a call; in ctypes it is about 25 us, as long as the small shapes take on the
 GPU).  It returns None for anything it does not take; the ctypes path below then runs, and says what is wrong.  Where the
 compiled part is missing or does not fit the interpreter and its PyTorch, every call takes the ctypes path (with a warning).
@@ -21,14 +21,16 @@ LIB_PATH = os.path.join(_HERE, "libcsr_hip.so")
 NATIVE_PATH = os.path.join(_HERE, "_csr_torch.so")
 
 CSR_OK, CSR_ERR_INVALID_ARG, CSR_ERR_UNSUPPORTED, CSR_ERR_WORKSPACE, CSR_ERR_DEVICE = range(5)
-CSR_F32, CSR_F16 = 0, 1
+CSR_F32, CSR_F16, CSR_BF16 = 0, 1, 2
 CSR_I32, CSR_I16 = 0, 1
 CSR_ENCODE_AUTO, CSR_ENCODE_VALU, CSR_ENCODE_MFMA, CSR_ENCODE_SPLIT, CSR_ENCODE_RESIDENT, CSR_ENCODE_GRAM, CSR_ENCODE_WIDE = range(7)
 CSR_FLAG_CLOSED_LOOP, CSR_FLAG_NO_WAIT = 1, 0x100
+CSR_FLAG_NOT_CAUSAL = 1
 
 EXPORTS = ("csr_version", "csr_last_error", "csr_code_bytes", "csr_encode_workspace_bytes",
            "csr_encode", "csr_decode_workspace_bytes", "csr_decode_attn", "csr_reconstruct", "csr_atom_norms2",
-           "csr_gram_bytes", "csr_gram_build", "csr_decode_attn_static", "csr_check_codes")
+           "csr_gram_bytes", "csr_gram_build", "csr_decode_attn_static", "csr_check_codes",
+           "csr_q4_bytes", "csr_q4_write", "csr_q4_read", "csr_q4_attn_workspace_bytes", "csr_q4_attn")
 STATIC_SCRATCH_BYTES = 16 << 20   # CSR_STATIC_SCRATCH_BYTES of include/csr.h
 
 
@@ -60,6 +62,23 @@ class DecodeDesc(ctypes.Structure):
                 ("coef_dtype", ctypes.c_int32), ("idx_dtype", ctypes.c_int32),
                 ("out_dtype", ctypes.c_int32), ("flags", ctypes.c_uint32),
                 ("rope_base", ctypes.c_float), ("rope_layout", ctypes.c_int32), ("rope_pos0", ctypes.c_int64)]
+
+
+class Q4RowsDesc(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("n", ctypes.c_int64), ("T", ctypes.c_int64),
+                ("d", ctypes.c_int32), ("group", ctypes.c_int32), ("x_dtype", ctypes.c_int32),
+                ("x_stride_b", ctypes.c_int64), ("x_stride_h", ctypes.c_int64), ("x_stride_t", ctypes.c_int64),
+                ("out_dtype", ctypes.c_int32), ("out_stride_b", ctypes.c_int64), ("out_stride_h", ctypes.c_int64),
+                ("out_stride_t", ctypes.c_int64), ("pos0", ctypes.c_int64), ("flags", ctypes.c_uint32)]
+
+
+class Q4AttnDesc(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("Tq", ctypes.c_int32),
+                ("T", ctypes.c_int64), ("d", ctypes.c_int32), ("group_k", ctypes.c_int32), ("group_v", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("q_dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32),
+                ("q_stride_b", ctypes.c_int64), ("q_stride_h", ctypes.c_int64), ("q_stride_t", ctypes.c_int64),
+                ("out_stride_b", ctypes.c_int64), ("out_stride_h", ctypes.c_int64), ("out_stride_t", ctypes.c_int64),
+                ("flags", ctypes.c_uint32)]
 
 
 class CsrError(RuntimeError):
@@ -104,13 +123,23 @@ def lib():
         L.csr_decode_attn.argtypes = [ctypes.POINTER(DecodeDesc)] + [vp] * 10 + [sz, vp]
         L.csr_decode_attn_static.restype = ctypes.c_int
         L.csr_decode_attn_static.argtypes = [ctypes.POINTER(DecodeDesc)] + [vp] * 9 + [vp]
+        L.csr_q4_bytes.restype = sz
+        L.csr_q4_bytes.argtypes = [ctypes.c_int32] * 2
+        L.csr_q4_write.restype = ctypes.c_int
+        L.csr_q4_write.argtypes = ([ctypes.POINTER(Q4RowsDesc)] + [vp] * 4) * 2 + [vp] * 3
+        L.csr_q4_read.restype = ctypes.c_int
+        L.csr_q4_read.argtypes = [ctypes.POINTER(Q4RowsDesc)] + [vp] * 6
+        L.csr_q4_attn_workspace_bytes.restype = sz
+        L.csr_q4_attn_workspace_bytes.argtypes = [ctypes.POINTER(Q4AttnDesc)]
+        L.csr_q4_attn.restype = ctypes.c_int
+        L.csr_q4_attn.argtypes = [ctypes.POINTER(Q4AttnDesc)] + [vp] * 9 + [sz, vp]
         _lib = L
     return _lib
 
 
 class _CtypesOnly:
     """Stands in for the compiled marshalling where it cannot be loaded: takes no call."""
-    encode = decode = reconstruct = staticmethod(lambda *_: None)
+    encode = decode = reconstruct = q4_write = q4_read = q4_attn = staticmethod(lambda *_: None)
 
 
 _native = None
@@ -125,7 +154,8 @@ def _load_native():
         module = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(module)
         module.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in
-                      (L.csr_encode_workspace_bytes, L.csr_encode, L.csr_decode_workspace_bytes, L.csr_decode_attn, L.csr_reconstruct)))
+                      (L.csr_encode_workspace_bytes, L.csr_encode, L.csr_decode_workspace_bytes, L.csr_decode_attn, L.csr_reconstruct,
+                       L.csr_q4_write, L.csr_q4_read, L.csr_q4_attn_workspace_bytes, L.csr_q4_attn)))
     except ImportError as e:
         warnings.warn(f"{NATIVE_PATH} cannot be loaded ({e}): calls go through ctypes, about 25 us of host time each; build it "
                       "with `python -m paper_2412_11741_amd.build`", RuntimeWarning, stacklevel=3)
@@ -412,3 +442,176 @@ def csr_decode_attn_static(q, DK, idxK, coefK, DV, idxV, coefV, out, scale=0.0, 
     return csr_decode_attn(q, DK, idxK, coefK, DV, idxV, coefV, scale=scale, seq_lens=seq_lens, out=out,
                            out_dtype=out_dtype or out.dtype, rope_base=rope_base, rope_layout=rope_layout,
                            rope_pos0=rope_pos0, static_scratch=True)
+
+
+# ---- a cache held in 4 bits -------------------------------------------------------------------------------------------
+_Q4 = {torch.float32: CSR_F32, torch.float16: CSR_F16, torch.bfloat16: CSR_BF16}
+
+
+def csr_q4_bytes(d, group=64):
+    """Bytes that the 4-bit cache keeps per head vector of d channels with a scale per `group`; 0 on bad arguments."""
+    return int(lib().csr_q4_bytes(d, group))
+
+
+def csr_q4_alloc(B, Hkv, T, d, group=64, device="cuda"):
+    """An empty 4-bit cache of T rows: (codes uint8 [B, Hkv, T, d / 2], params fp16 [B, Hkv, d / group, T, 2]), zeros."""
+    if not csr_q4_bytes(d, group):
+        raise ValueError(f"d={d} must be 64 or 128, group={group} 32, 64 or 128 and at most d")
+    return (torch.zeros(B, Hkv, T, d // 2, dtype=torch.uint8, device=device),
+            torch.zeros(B, Hkv, d // group, T, 2, dtype=torch.float16, device=device))
+
+
+def _q4_cache(codes, params, name, like=None):
+    """(B, Hkv, T, d, group) of a cache's two tensors"""
+    for what, t, dt in (("codes", codes, torch.uint8), ("params", params, torch.float16)):
+        if _dev(t, what + name).dtype != dt or not t.is_contiguous():
+            raise ValueError(f"{what}{name} must be a contiguous {dt} tensor")
+    if codes.dim() != 4 or params.dim() != 5:
+        raise ValueError(f"expected codes{name} [B, Hkv, T, d / 2] and params{name} [B, Hkv, d / group, T, 2]")
+    B, Hkv, T, half = codes.shape
+    d, groups = 2 * half, params.shape[2]
+    if tuple(params.shape) != (B, Hkv, groups, T, 2) or groups < 1 or d % groups:
+        raise ValueError(f"params{name} {tuple(params.shape)} do not belong to codes{name} {tuple(codes.shape)}: expected [B, Hkv, d / group, T, 2]")
+    if like is not None and codes.shape != like.shape:
+        raise ValueError(f"codes{name} {tuple(codes.shape)} and codes {tuple(like.shape)} disagree in shape")
+    return B, Hkv, T, d, d // groups
+
+
+def _q4_dense(t, shape, name, dtype=None):
+    """A dense operand [B, H, n, d] of one of the three types, its rows contiguous"""
+    _dev(t, name)
+    if tuple(t.shape) != tuple(shape) or t.dtype not in _Q4 or (dtype is not None and t.dtype != dtype):
+        raise ValueError(f"{name} must have shape {tuple(shape)} and dtype {dtype or 'float16, bfloat16 or float32'}, got {tuple(t.shape)} {t.dtype}")
+    if t.stride(-1) != 1:
+        raise ValueError(f"{name} must be contiguous along d")
+    return t
+
+
+def _q4_lens(t, B, name):
+    if t is not None and (_dev(t, name).dtype != torch.int32 or t.numel() != B or not t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous int32 tensor [B]")
+    return t
+
+
+def _q4_device(*tensors):
+    """The device of all of them: the call runs there, on its current stream"""
+    devices = {t.device for t in tensors if t is not None}
+    if len(devices) != 1:
+        raise ValueError(f"tensors on several devices: {sorted(map(str, devices))}")
+    return torch.cuda.device(devices.pop())
+
+
+def _q4_rows_desc(X, out, B, Hkv, n, T, d, group, pos0, dtype):
+    xs, os = (t.stride() if t is not None else (0, 0, 0) for t in (X, out))
+    return Q4RowsDesc(B=B, Hkv=Hkv, n=n, T=T, d=d, group=group, x_dtype=_Q4[X.dtype] if X is not None else 0,
+                      x_stride_b=xs[0], x_stride_h=xs[1], x_stride_t=xs[2], out_dtype=_Q4[dtype],
+                      out_stride_b=os[0], out_stride_h=os[1], out_stride_t=os[2], pos0=int(pos0), flags=0)
+
+
+def csr_q4_write(K, codesK, paramsK, V=None, codesV=None, paramsV=None, pos0=0, pos=None, counts=None, values=False, outK=None, outV=None):
+    """Quantise rows K [B, Hkv, n, d] (fp16, bf16 or fp32, any strides of whole 16 bytes) - and V in the same launch - into 4-bit caches
+    (csr_q4_alloc).  Row t goes to cache row pos0 + pos[b] + t (`pos`: int32 [B]); of every sequence the first counts[b] rows
+    (int32 [B], all without) are written, and none outside the cache.  values=True, or outK / outV: returns what the cache now
+    stands for, in K's type (zeros where nothing was written) - one tensor, or one for each of K and V."""
+    done = (_native or _load_native()).q4_write(K, codesK, paramsK, V, codesV, paramsV, pos0, pos, counts, values, outK, outV)
+    if done is not None:
+        return done[0]
+    sides = [("K", K, codesK, paramsK, outK)]
+    if V is not None:
+        sides.append(("V", V, codesV, paramsV, outV))
+    elif any(t is not None for t in (codesV, paramsV, outV)):
+        raise ValueError("codesV, paramsV or outV without V")
+    if _dev(K, "K").dim() != 4:
+        raise ValueError("K must be [B, Hkv, n, d]")
+    if V is not None and (outK is None) != (outV is None):
+        raise ValueError("outK and outV: both or neither")
+    args, outs, kept = [], [], [pos, counts]
+    for name, X, codes, params, out in sides:
+        B, Hkv, T, d, group = _q4_cache(codes, params, name, codesK if name == "V" else None)
+        n = K.shape[2]
+        _q4_dense(X, (B, Hkv, n, d), name, K.dtype)
+        if out is None and values:
+            out = torch.empty((B, Hkv, n, d), dtype=K.dtype, device=K.device)
+        if out is not None:
+            _q4_dense(out, (B, Hkv, n, d), "out" + name, K.dtype)
+            outs.append(out)
+        args += [ctypes.byref(_q4_rows_desc(X, out, B, Hkv, n, T, d, group, pos0, K.dtype)), _ptr(X), _ptr(codes), _ptr(params), _ptr(out)]
+        kept += [X, codes, params, out]
+    _q4_lens(pos, B, "pos"); _q4_lens(counts, B, "counts")
+    with _q4_device(*kept):
+        _check(lib().csr_q4_write(*args, *([None] * (10 - len(args))), _ptr(pos), _ptr(counts), _stream()))
+    return None if not outs else outs[0] if V is None else tuple(outs)
+
+
+def csr_q4_read(codes, params, n=None, pos0=0, pos=None, counts=None, out=None, out_dtype=None):
+    """Rows of a 4-bit cache as dense vectors: out[b, h, t] is cache row pos0 + pos[b] + t, for t < counts[b] and rows inside the
+    cache, and zeros elsewhere.  n: rows of `out`, by default as many as the cache has from pos0 on; out_dtype fp16 by default."""
+    done = (_native or _load_native()).q4_read(codes, params, n, pos0, pos, counts, out, out_dtype)
+    if done is not None:
+        return done
+    B, Hkv, T, d, group = _q4_cache(codes, params, "")
+    if out is not None and n is None and out.dim() == 4:
+        n = out.shape[2]
+    n = max(0, T - max(0, pos0)) if n is None else n
+    dtype = out_dtype or (out.dtype if out is not None else torch.float16)
+    if dtype not in _Q4 or n < 0:
+        raise ValueError("out_dtype must be float16, bfloat16 or float32, n >= 0")
+    if out is None:
+        out = torch.empty((B, Hkv, n, d), dtype=dtype, device=codes.device)
+    _q4_dense(out, (B, Hkv, n, d), "out", dtype)
+    _q4_lens(pos, B, "pos"); _q4_lens(counts, B, "counts")
+    desc = _q4_rows_desc(None, out, B, Hkv, n, T, d, group, pos0, dtype)
+    with _q4_device(codes, params, out, pos, counts):
+        _check(lib().csr_q4_read(ctypes.byref(desc), _ptr(codes), _ptr(params), _ptr(out), _ptr(pos), _ptr(counts), _stream()))
+    return out
+
+
+def q4_attn_desc(q, codesK, paramsK, paramsV, out, scale=0.0, causal=True):
+    """Descriptor from tensor shapes; q and out [B, Hq, Tq, d]."""
+    B, Hq, Tq, d = q.shape
+    qs, os = q.stride(), out.stride()
+    return Q4AttnDesc(B=B, Hq=Hq, Hkv=codesK.shape[1], Tq=Tq, T=codesK.shape[2], d=d, group_k=d // paramsK.shape[2], group_v=d // paramsV.shape[2],
+                      scale=float(scale), q_dtype=_Q4[q.dtype], out_dtype=_Q4[out.dtype], q_stride_b=qs[0], q_stride_h=qs[1], q_stride_t=qs[2],
+                      out_stride_b=os[0], out_stride_h=os[1], out_stride_t=os[2], flags=0 if causal else CSR_FLAG_NOT_CAUSAL)
+
+
+def csr_q4_attn_workspace_bytes(desc):
+    n = lib().csr_q4_attn_workspace_bytes(ctypes.byref(desc))
+    if n == ctypes.c_size_t(-1).value:
+        raise CsrError(CSR_ERR_INVALID_ARG, last_error())
+    return int(n)
+
+
+def csr_q4_attn(q, codesK, paramsK, codesV, paramsV, scale=0.0, seq_lens=None, q_lens=None, causal=True, out=None, out_dtype=None,
+                workspace=None):
+    """Softmax attention over a 4-bit cache.  q [B, Hq, d] (one query token per sequence) or [B, Hq, Tq, d] (its last Tq tokens; with
+    `q_lens` int32 [B] the first q_lens[b] of them, the rest yield zeros) -> out of q's shape and, without out_dtype, its type.
+    Query i of qn stands at token len - qn + i of its sequence and sees the tokens up to it (causal=False: all of them);
+    len = seq_lens[b] (int32 [B]), or all rows of the cache."""
+    done = (_native or _load_native()).q4_attn(q, codesK, paramsK, codesV, paramsV, scale, seq_lens, q_lens, causal, out, out_dtype, workspace)
+    if done is not None:
+        return done
+    B, Hkv, T, d, _ = _q4_cache(codesK, paramsK, "K")
+    _q4_cache(codesV, paramsV, "V", codesK)
+    if _dev(q, "q").dim() not in (3, 4):
+        raise ValueError("q must be [B, Hq, d] or [B, Hq, Tq, d]")
+    q4 = q if q.dim() == 4 else q.unsqueeze(2)
+    _q4_dense(q4, (B, q.shape[1], q4.shape[2], d), "q")
+    dtype = out_dtype or (out.dtype if out is not None else q.dtype)
+    if dtype not in _Q4:
+        raise ValueError("out_dtype must be float16, bfloat16 or float32")
+    if out is None:
+        out = torch.empty(q.shape, dtype=dtype, device=q.device)
+    if _dev(out, "out").shape != q.shape:
+        raise ValueError(f"out must have q's shape {tuple(q.shape)}")
+    o4 = _q4_dense(out if q.dim() == 4 else out.unsqueeze(2), q4.shape, "out", dtype)
+    _q4_lens(seq_lens, B, "seq_lens"); _q4_lens(q_lens, B, "q_lens")
+    desc = q4_attn_desc(q4, codesK, paramsK, paramsV, o4, scale, causal)
+    with _q4_device(q, codesK, paramsK, codesV, paramsV, seq_lens, q_lens, out, workspace):
+        need = csr_q4_attn_workspace_bytes(desc)
+        if workspace is None and need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        _check(lib().csr_q4_attn(ctypes.byref(desc), _ptr(q), _ptr(codesK), _ptr(paramsK), _ptr(codesV), _ptr(paramsV), _ptr(seq_lens),
+                                 _ptr(q_lens), _ptr(out), _ptr(workspace),
+                                 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream()))
+    return out

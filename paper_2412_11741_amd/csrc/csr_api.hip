@@ -266,6 +266,94 @@ void fit_decode_plan(size_t bytes, csr::DecodePlan *p)
     p->total_bytes = p->table_bytes;
 }
 
+// ---- the cache held in 4 bits ---------------------------------------------------------------------------------------
+bool valid_q4_dtype(int32_t v) { return valid_dtype(v) || v == CSR_BF16; }
+bool valid_q4_shape(int32_t d, int32_t group)
+{
+    return (d == 64 || d == 128) && (group == 32 || group == 64 || group == 128) && group <= d;
+}
+
+// Strides of a dense operand: whole 16-byte steps, never backwards; an output's rows do not overlap
+csr_status check_q4_strides(const char *call, const char *what, const int64_t (&stride)[3], const int64_t (&size)[3], int32_t dtype,
+                            int32_t d, bool output)
+{
+    const int64_t step = dtype == CSR_F32 ? 4 : 8;   // elements of 16 bytes
+    for (int k = 0; k < 3; ++k) {
+        if (size[k] <= 1) continue;
+        if (stride[k] < 0 || stride[k] % step != 0)
+            return fail(CSR_ERR_INVALID_ARG, "%s: strides of %s must be multiples of 16 bytes and not negative (got %lld)", call, what, (long long)stride[k]);
+        if (output && stride[k] < d)
+            return fail(CSR_ERR_INVALID_ARG, "%s: strides of %s must be at least d=%d (got %lld)", call, what, d, (long long)stride[k]);
+        if (stride[k] > ((int64_t)1 << 48) / size[k])
+            return fail(CSR_ERR_UNSUPPORTED, "%s: strides of %s are too large", call, what);
+    }
+    return CSR_OK;
+}
+
+csr_status check_q4_rows(const char *call, const csr_q4_rows_desc *d, bool reads_x, bool writes_out)
+{
+    if (!d) return fail(CSR_ERR_INVALID_ARG, "%s: descriptor is NULL", call);
+    if (d->flags != 0) return fail(CSR_ERR_INVALID_ARG, "%s: flags must be 0", call);
+    if (d->B < 0 || d->Hkv < 1 || d->n < 0 || d->T < 0)
+        return fail(CSR_ERR_INVALID_ARG, "%s: B=%d, n=%lld and T=%lld must be >= 0, Hkv=%d >= 1", call, d->B, (long long)d->n, (long long)d->T, d->Hkv);
+    if ((writes_out && !valid_q4_dtype(d->out_dtype)) || (reads_x && !valid_q4_dtype(d->x_dtype)))
+        return fail(CSR_ERR_INVALID_ARG, "%s: unknown dtype", call);
+    if (!valid_q4_shape(d->d, d->group))
+        return fail(CSR_ERR_UNSUPPORTED, "%s: d=%d must be 64 or 128, group=%d 32, 64 or 128 and at most d", call, d->d, d->group);
+    if (d->T > (int64_t)1 << 20) return fail(CSR_ERR_UNSUPPORTED, "%s: T above 2^20", call);
+    if (d->pos0 > (int64_t)1 << 40 || d->pos0 < -((int64_t)1 << 40)) return fail(CSR_ERR_INVALID_ARG, "%s: pos0 outside +-2^40", call);
+    if (d->n > 0x3fffffff || (d->B > 0 && (int64_t)d->B * d->Hkv > 0x3fffffff / (d->n > 0 ? d->n : 1)))
+        return fail(CSR_ERR_UNSUPPORTED, "%s: more than 2^30 rows in one call", call);
+    const int64_t size[3] = {d->B, d->Hkv, d->n}, xs[3] = {d->x_stride_b, d->x_stride_h, d->x_stride_t},
+                  os[3] = {d->out_stride_b, d->out_stride_h, d->out_stride_t};
+    csr_status st = reads_x ? check_q4_strides(call, "X", xs, size, d->x_dtype, d->d, false) : CSR_OK;
+    return st != CSR_OK || !writes_out ? st : check_q4_strides(call, "out", os, size, d->out_dtype, d->d, true);
+}
+
+csr::Q4RowsSide q4_side(const csr_q4_rows_desc &d, const void *x, void *codes, void *params, void *out)
+{
+    return {x, codes, params, out, {d.x_stride_b, d.x_stride_h, d.x_stride_t}, {d.out_stride_b, d.out_stride_h, d.out_stride_t}, d.group};
+}
+
+csr_status check_q4_pointers(const char *call, const void *codes, const void *params, const int32_t *pos, const int32_t *counts)
+{
+    if (!aligned(codes, 16) || !aligned(params, 4)) return fail(CSR_ERR_INVALID_ARG, "%s: codes must be 16-byte aligned, params 4-byte", call);
+    if (!aligned(pos, 4) || !aligned(counts, 4)) return fail(CSR_ERR_INVALID_ARG, "%s: pos or counts misaligned", call);
+    return CSR_OK;
+}
+
+csr_status check_q4_attn(const csr_q4_attn_desc *d, csr::Q4AttnArgs *args, csr::Q4AttnPlan *plan)
+{
+    if (!d) return fail(CSR_ERR_INVALID_ARG, "csr_q4_attn: descriptor is NULL");
+    if (d->flags & ~CSR_FLAG_NOT_CAUSAL) return fail(CSR_ERR_INVALID_ARG, "csr_q4_attn: unknown flags %#x", d->flags);
+    if (d->B < 0 || d->Tq < 0 || d->T < 0)
+        return fail(CSR_ERR_INVALID_ARG, "csr_q4_attn: B=%d Tq=%d T=%lld must be >= 0", d->B, d->Tq, (long long)d->T);
+    if (d->Hq < 1 || d->Hkv < 1 || d->Hq % d->Hkv != 0)
+        return fail(CSR_ERR_INVALID_ARG, "csr_q4_attn: Hq=%d must be a positive multiple of Hkv=%d", d->Hq, d->Hkv);
+    if (!valid_q4_dtype(d->q_dtype) || !valid_q4_dtype(d->out_dtype)) return fail(CSR_ERR_INVALID_ARG, "csr_q4_attn: unknown dtype");
+    if (!(d->scale >= 0.0f) || std::isinf(d->scale))
+        return fail(CSR_ERR_INVALID_ARG, "csr_q4_attn: scale must be finite and >= 0 (0 selects 1/sqrt(d))");
+    if (!valid_q4_shape(d->d, d->group_k) || !valid_q4_shape(d->d, d->group_v))
+        return fail(CSR_ERR_UNSUPPORTED, "csr_q4_attn: d=%d must be 64 or 128, group_k=%d and group_v=%d 32, 64 or 128 and at most d", d->d, d->group_k, d->group_v);
+    if (d->T > (int64_t)1 << 20) return fail(CSR_ERR_UNSUPPORTED, "csr_q4_attn: T above 2^20");
+    if (d->B > 65535 || d->Hkv > 65535 || (d->B > 0 && (int64_t)d->Hq * (d->Tq > 0 ? d->Tq : 1) > (int64_t)0x0fffffff / d->B))
+        return fail(CSR_ERR_UNSUPPORTED, "csr_q4_attn: B or Hkv above 65535, or more than 2^28 query rows");
+    const int64_t size[3] = {d->B, d->Hq, d->Tq}, qs[3] = {d->q_stride_b, d->q_stride_h, d->q_stride_t},
+                  os[3] = {d->out_stride_b, d->out_stride_h, d->out_stride_t};
+    csr_status st = check_q4_strides("csr_q4_attn", "q", qs, size, d->q_dtype, d->d, false);
+    if (st == CSR_OK) st = check_q4_strides("csr_q4_attn", "out", os, size, d->out_dtype, d->d, true);
+    if (st != CSR_OK) return st;
+    csr::Q4AttnArgs a{};
+    a.B = d->B; a.Hq = d->Hq; a.Hkv = d->Hkv; a.G = d->Hq / d->Hkv; a.Tq = d->Tq; a.T = d->T;
+    a.d = d->d; a.group_k = d->group_k; a.group_v = d->group_v; a.q_dtype = d->q_dtype; a.out_dtype = d->out_dtype;
+    a.scale = d->scale > 0.0f ? d->scale : 1.0f / std::sqrt((float)d->d);
+    a.causal = !(d->flags & CSR_FLAG_NOT_CAUSAL);
+    for (int k = 0; k < 3; ++k) { a.q_stride[k] = qs[k]; a.out_stride[k] = os[k]; }
+    csr::plan_q4_attn(a, plan);
+    *args = a;
+    return CSR_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -498,6 +586,98 @@ csr_status csr_decode_attn_static(const csr_decode_desc *desc, const void *q, co
     // Nothing in the scratch has to start at zero: every launch writes what the next one reads (chunk histograms
     // of chunks without tokens are never read), so the previous call's contents are simply overwritten.
     return decode_run(desc, p, q, DK, idxK, coefK, DV, idxV, coefV, seq_lens, out, ws, hip_stream);
+}
+
+size_t csr_q4_bytes(int32_t d, int32_t group)
+{
+    return valid_q4_shape(d, group) ? (size_t)d / 2 + 4 * (size_t)(d / group) : 0;
+}
+
+csr_status csr_q4_write(const csr_q4_rows_desc *desc, const void *X, void *codes, void *params, void *out,
+                        const csr_q4_rows_desc *desc2, const void *X2, void *codes2, void *params2, void *out2,
+                        const int32_t *pos, const int32_t *counts, void *hip_stream)
+{
+    csr_status st = check_q4_rows("csr_q4_write", desc, true, out != nullptr);
+    if (st == CSR_OK && desc2) st = check_q4_rows("csr_q4_write", desc2, true, out2 != nullptr);
+    if (st != CSR_OK) return st;
+    if (!desc2 && (X2 || codes2 || params2 || out2)) return fail(CSR_ERR_INVALID_ARG, "csr_q4_write: a second tensor without its descriptor");
+    if (desc2 && (desc2->B != desc->B || desc2->Hkv != desc->Hkv || desc2->n != desc->n || desc2->T != desc->T || desc2->d != desc->d ||
+                  desc2->x_dtype != desc->x_dtype || desc2->out_dtype != desc->out_dtype || desc2->pos0 != desc->pos0))
+        return fail(CSR_ERR_INVALID_ARG, "csr_q4_write: the two descriptors may differ in group and strides only");
+    if (desc2 && (out == nullptr) != (out2 == nullptr)) return fail(CSR_ERR_INVALID_ARG, "csr_q4_write: out and out2 must both be given or both be NULL");
+    if (desc->B == 0 || desc->n == 0) return CSR_OK;
+    if (!X || (desc2 && !X2)) return fail(CSR_ERR_INVALID_ARG, "csr_q4_write: NULL data pointer");
+    if (desc->T > 0 && (!codes || !params || (desc2 && (!codes2 || !params2)))) return fail(CSR_ERR_INVALID_ARG, "csr_q4_write: NULL cache pointer with T > 0");
+    if (!aligned(X, 16) || !aligned(out, 16) || !aligned(X2, 16) || !aligned(out2, 16))
+        return fail(CSR_ERR_INVALID_ARG, "csr_q4_write: X and out must be 16-byte aligned");
+    st = check_q4_pointers("csr_q4_write", codes, params, pos, counts);
+    if (st == CSR_OK) st = check_q4_pointers("csr_q4_write", codes2, params2, pos, counts);
+    if (st != CSR_OK) return st;
+    csr::Q4RowsArgs a{};
+    a.side[0] = q4_side(*desc, X, codes, params, out);
+    if (desc2) a.side[1] = q4_side(*desc2, X2, codes2, params2, out2);
+    a.B = desc->B; a.Hkv = desc->Hkv; a.n = desc->n; a.T = desc->T; a.d = desc->d;
+    a.x_dtype = desc->x_dtype; a.out_dtype = desc->out_dtype; a.pos0 = desc->pos0; a.pos = pos; a.counts = counts;
+    a.stream = static_cast<hipStream_t>(hip_stream);
+    const hipError_t e = csr::launch_q4_write(a, desc2 ? 2 : 1);
+    if (e != hipSuccess) return fail(CSR_ERR_DEVICE, "csr_q4_write: %s", hipGetErrorString(e));
+    return CSR_OK;
+}
+
+csr_status csr_q4_read(const csr_q4_rows_desc *desc, const void *codes, const void *params, void *out, const int32_t *pos,
+                       const int32_t *counts, void *hip_stream)
+{
+    csr_status st = check_q4_rows("csr_q4_read", desc, false, true);
+    if (st != CSR_OK) return st;
+    if (desc->B == 0 || desc->n == 0) return CSR_OK;
+    if (!out) return fail(CSR_ERR_INVALID_ARG, "csr_q4_read: NULL output pointer");
+    if (desc->T > 0 && (!codes || !params)) return fail(CSR_ERR_INVALID_ARG, "csr_q4_read: NULL cache pointer with T > 0");
+    if (!aligned(out, 16)) return fail(CSR_ERR_INVALID_ARG, "csr_q4_read: out must be 16-byte aligned");
+    st = check_q4_pointers("csr_q4_read", codes, params, pos, counts);
+    if (st != CSR_OK) return st;
+    csr::Q4RowsArgs a{};
+    a.side[0] = q4_side(*desc, nullptr, const_cast<void *>(codes), const_cast<void *>(params), out);
+    a.B = desc->B; a.Hkv = desc->Hkv; a.n = desc->n; a.T = desc->T; a.d = desc->d;
+    a.out_dtype = desc->out_dtype; a.pos0 = desc->pos0; a.pos = pos; a.counts = counts;
+    a.stream = static_cast<hipStream_t>(hip_stream);
+    const hipError_t e = csr::launch_q4_read(a);
+    if (e != hipSuccess) return fail(CSR_ERR_DEVICE, "csr_q4_read: %s", hipGetErrorString(e));
+    return CSR_OK;
+}
+
+size_t csr_q4_attn_workspace_bytes(const csr_q4_attn_desc *desc)
+{
+    csr::Q4AttnArgs a{};
+    csr::Q4AttnPlan p{};
+    if (check_q4_attn(desc, &a, &p) != CSR_OK) return (size_t)-1;
+    return p.total_bytes;
+}
+
+csr_status csr_q4_attn(const csr_q4_attn_desc *desc, const void *q, const void *codesK, const void *paramsK,
+                       const void *codesV, const void *paramsV, const int32_t *seq_lens, const int32_t *q_lens, void *out,
+                       void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    csr::Q4AttnArgs a{};
+    csr::Q4AttnPlan p{};
+    csr_status st = check_q4_attn(desc, &a, &p);
+    if (st != CSR_OK) return st;
+    if (desc->B == 0 || desc->Tq == 0) return CSR_OK;
+    if (!q || !out) return fail(CSR_ERR_INVALID_ARG, "csr_q4_attn: NULL data pointer");
+    if (desc->T > 0 && (!codesK || !paramsK || !codesV || !paramsV)) return fail(CSR_ERR_INVALID_ARG, "csr_q4_attn: NULL cache pointer with T > 0");
+    if (!aligned(q, 16) || !aligned(out, 16)) return fail(CSR_ERR_INVALID_ARG, "csr_q4_attn: q and out must be 16-byte aligned");
+    st = check_q4_pointers("csr_q4_attn", codesK, paramsK, seq_lens, q_lens);
+    if (st == CSR_OK) st = check_q4_pointers("csr_q4_attn", codesV, paramsV, nullptr, nullptr);
+    if (st != CSR_OK) return st;
+    if (p.total_bytes > 0 && (!workspace || workspace_bytes < p.total_bytes || !aligned(workspace, 256)))
+        return fail(CSR_ERR_WORKSPACE, "csr_q4_attn: workspace of %zu bytes (256-byte aligned) required, got %zu", p.total_bytes,
+                    workspace ? workspace_bytes : (size_t)0);
+    a.q = q; a.codesK = codesK; a.paramsK = paramsK; a.codesV = codesV; a.paramsV = paramsV;
+    a.seq_lens = seq_lens; a.q_lens = q_lens; a.out = out;
+    a.workspace = workspace;
+    a.stream = static_cast<hipStream_t>(hip_stream);
+    const hipError_t e = csr::launch_q4_attn(a, p);
+    if (e != hipSuccess) return fail(CSR_ERR_DEVICE, "csr_q4_attn: %s", hipGetErrorString(e));
+    return CSR_OK;
 }
 
 }  // extern "C"

@@ -155,4 +155,46 @@ hipError_t launch_decode_direct(const DecodeArgs &a, const DecodePlan &p);
 bool decode_rope_shape_supported(int32_t d, int32_t N, int32_t sK, int32_t snK);
 hipError_t launch_stream_rope(const DecodeArgs &a, const DecodePlan &p, float *hist, float *ml);
 
+// ---- the cache held in 4 bits -----------------------------------------------------------------
+struct Q4RowsSide {
+    const void *x;
+    void *codes, *params, *out;
+    int64_t x_stride[3], out_stride[3];  // sequence, head, token; elements
+    int32_t group;
+};
+struct Q4RowsArgs {
+    Q4RowsSide side[2];
+    int32_t B, Hkv;
+    int64_t n, T;
+    int32_t d, x_dtype, out_dtype;
+    int64_t pos0;
+    const int32_t *pos, *counts;
+    hipStream_t stream;
+};
+hipError_t launch_q4_write(const Q4RowsArgs &a, int sides);  // sides: 1 or 2
+hipError_t launch_q4_read(const Q4RowsArgs &a);
+
+struct Q4AttnArgs {
+    const void *q;
+    const void *codesK, *paramsK, *codesV, *paramsV;
+    const int32_t *seq_lens, *q_lens;
+    void *out;
+    int32_t B, Hq, Hkv, G, Tq;
+    int64_t T;
+    int32_t d, group_k, group_v, q_dtype, out_dtype;
+    float scale;
+    bool causal;
+    int64_t q_stride[3], out_stride[3];  // sequence, head, token; elements
+    void *workspace;
+    hipStream_t stream;
+};
+struct Q4AttnPlan {
+    int32_t row_tiles;   // tiles of 16 query rows (query token, head) that a workgroup takes
+    int32_t row_blocks;  // workgroups along the query rows of a KV head
+    int32_t splits;      // ... and along its tokens
+    size_t off_ml, total_bytes;
+};
+void plan_q4_attn(const Q4AttnArgs &a, Q4AttnPlan *p);  // shape, types and causal of a
+hipError_t launch_q4_attn(const Q4AttnArgs &a, const Q4AttnPlan &p);
+
 }  // namespace csr

@@ -1,0 +1,440 @@
+// Attention over the 4-bit cache: a few query rows per KV head.
+//
+// A query row is a (query token, query head) of the KV head; row r is query token r / G, head r % G of the group.  The cache is
+// read once per block of rows and bounds the time, so everything else is arranged around wide requests in flight: a wave
+// streams tokens, 32 at a time, straight into registers, with the next 32 requested before these are used, and shares nothing
+// with other waves until the end.
+//
+// For 32 tokens: S^T = K q^T and O^T += V^T p^T on the matrix cores (16x16x32, fp16 in, fp32 out).  With the tokens as rows of
+// S^T and channels as rows of O^T a query row stays in the same 16th of the lanes throughout: its maximum, sum and
+// probabilities never cross lanes but for the maximum.  Which of the instruction's 32 contraction places means which channel
+// (S^T) or which token (O^T) is free as long as both operands agree, so
+//   - lane (m, kg) takes the channels 32 kg .. of token m's key (d / 4 of them: one or two words, one group of the scale);
+//   - a lane's four scores of either half of the 32 tokens are tokens 8 kg .. 8 kg + 7 and go into the next product as they are;
+//   - lane (m, kg) takes channels (d / 16) m .. of the values of tokens 8 kg .. 8 kg + 7: two tokens' words are cut into halves and
+//     joined, and every nibble pair is then one channel of two tokens.
+// Probabilities are relative to 2^13 below the running maximum (and the maximum is only moved when it is passed by 2^2), so that
+// as two fp16 - the value and what it lacks - they keep 22 bits down to 2^-27 of the largest, and the rest to 2^-37.
+#include <cmath>
+#include <type_traits>
+
+#include "q4_common.h"
+
+namespace csr {
+namespace {
+
+using namespace q4;
+
+constexpr int kStep = 32;          // tokens of a wave's turn
+constexpr float kShift = 13.0f;    // p = 2^(score - maximum + kShift)
+constexpr float kSlack = 2.0f;     // a maximum may lag this far behind: p <= 2^15
+constexpr float kNone = -1e30f;    // a maximum before any token
+
+__device__ __forceinline__ float4v mfma(half8v a, half8v b, float4v c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+__device__ __forceinline__ half8v join(half2v a, half2v b, half2v c, half2v d)
+{
+    return half8v{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+struct AttnKernelArgs {
+    Q4AttnArgs a;
+    int32_t splits, row_blocks, rows;
+    float *acc, *ml;
+};
+
+// Tokens that the queries of a block see: [0, end) by some, [0, all) by all
+struct Sight {
+    int len, qn, end, all;
+};
+__device__ __forceinline__ Sight sight_of(const Q4AttnArgs &a, int b, int row0, int row_end)
+{
+    Sight s;
+    s.len = (int)a.T;
+    if (a.seq_lens) s.len = max(0, min(a.seq_lens[b], (int)a.T));
+    s.qn = a.q_lens ? max(0, min(a.q_lens[b], a.Tq)) : a.Tq;
+    const int first = row0 / a.G, last = min((row_end - 1) / a.G, s.qn - 1);
+    if (first >= s.qn) { s.end = s.all = 0; return s; }
+    s.end = a.causal ? max(0, s.len - s.qn + last + 1) : s.len;
+    s.all = (row_end - 1) / a.G >= s.qn ? 0 : a.causal ? max(0, s.len - s.qn + first + 1) : s.len;
+    return s;
+}
+// The last token that query row r sees, -1 for none
+__device__ __forceinline__ int limit_of(const Q4AttnArgs &a, const Sight &s, int r, int rows)
+{
+    const int i = r / a.G;
+    if (r >= rows || i >= s.qn) return -1;
+    return a.causal ? s.len - s.qn + i : s.len - 1;
+}
+
+__device__ __forceinline__ void store_out(const Q4AttnArgs &a, int64_t at, float v)
+{
+    if (a.out_dtype == CSR_F32) static_cast<float *>(a.out)[at] = v;
+    else if (a.out_dtype == CSR_F16) static_cast<_Float16 *>(a.out)[at] = (_Float16)v;
+    else static_cast<uint16_t *>(a.out)[at] = float_to_bf16(v);
+}
+
+// Eight channels of a query row as floats
+__device__ __forceinline__ void load_q8(const Q4AttnArgs &a, int64_t at, float (&v)[8])
+{
+    if (a.q_dtype == CSR_F32) {
+        const float4v *f = reinterpret_cast<const float4v *>(static_cast<const float *>(a.q) + at);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = f[k / 4][k % 4];
+    } else {
+        const uint4v w = *reinterpret_cast<const uint4v *>(static_cast<const uint16_t *>(a.q) + at);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            v[2 * k] = a.q_dtype == CSR_F16 ? (float)as_half2(w[k])[0] : __uint_as_float(w[k] << 16);
+            v[2 * k + 1] = a.q_dtype == CSR_F16 ? (float)as_half2(w[k])[1] : __uint_as_float(w[k] & 0xffff0000u);
+        }
+    }
+}
+
+// The codes and parameters of a wave's 32 tokens, as requested
+template <int D> struct Raw {
+    uint32_t kc[2][D / 32], kp[2], vc[8], vp[8];
+};
+
+template <int D>
+__device__ __forceinline__ void request(Raw<D> &r, const uint8_t *kc, const uint32_t *kp, const uint8_t *vc, const uint32_t *vp, int tb, int T, int m, int kg)
+{
+    const int last = T - 1;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const int t = min(tb + 8 * (m >> 2) + (m & 3) + 4 * u, last);
+        if constexpr (D == 128) {
+            const uint4v w = *reinterpret_cast<const uint4v *>(kc + (size_t)t * 64 + kg * 16);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) r.kc[u][k] = w[k];
+        } else {
+            const uint2v w = *reinterpret_cast<const uint2v *>(kc + (size_t)t * 32 + kg * 8);
+            r.kc[u][0] = w[0];
+            r.kc[u][1] = w[1];
+        }
+        r.kp[u] = kp[t];
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int t = min(tb + 8 * kg + j, last);
+        if constexpr (D == 128) r.vc[j] = *reinterpret_cast<const uint32_t *>(vc + (size_t)t * 64 + m * 4);
+        else r.vc[j] = *reinterpret_cast<const uint16_t *>(vc + (size_t)t * 32 + m * 2);
+        r.vp[j] = vp[t];
+    }
+}
+
+// QMODE: csr_dtype of q.  NR: tiles of 16 query rows.  W: waves.
+template <int D, int QMODE, int NR, int W>
+__global__ __launch_bounds__(64 * W) void q4_stream_kernel(AttnKernelArgs ka)
+{
+    constexpr int KM = D / 32;   // matrix instructions along a key's channels
+    constexpr int UC = D / 16;   // channels of a lane's values
+    constexpr bool kTwo = QMODE == CSR_F32;
+    const Q4AttnArgs &a = ka.a;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, kg = lane >> 4;
+    int x = blockIdx.x;
+    const int rb = x % ka.row_blocks;
+    x /= ka.row_blocks;
+    const int split = x % ka.splits, bh = x / ka.splits, b = bh / a.Hkv, h = bh - b * a.Hkv;
+    const int row0 = rb * 16 * NR, row_end = min(row0 + 16 * NR, ka.rows);
+    const Sight s = sight_of(a, b, row0, row_end);
+    const int per = ((s.end + ka.splits - 1) / ka.splits + kStep * W - 1) / (kStep * W) * (kStep * W);
+    const int begin = min(split * per, s.end), end = min(begin + per, s.end);
+
+    // the queries: fp16, and what that lacks; in units that leave no loss to bf16
+    half8v qh[NR][KM], ql[kTwo ? NR : 1][KM];
+    float unit[NR];
+    int limit[NR];
+#pragma unroll
+    for (int t = 0; t < NR; ++t) {
+        const int r = row0 + 16 * t + m;
+        limit[t] = limit_of(a, s, r, ka.rows);
+        unit[t] = a.scale * 1.44269504088896340736f;
+        float v[KM][8], top = 0.0f;
+        const int rr = min(r, ka.rows - 1), i = rr / a.G, hq = h * a.G + rr - i * a.G;
+        const int64_t at = (int64_t)b * a.q_stride[0] + (int64_t)hq * a.q_stride[1] + (int64_t)i * a.q_stride[2] + kg * (D / 4);
+#pragma unroll
+        for (int k = 0; k < KM; ++k) {
+            load_q8(a, at + 8 * k, v[k]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(v[k][j]));
+        }
+        if constexpr (QMODE != CSR_F16) {
+            top = fmaxf(top, __shfl_xor(top, 16, 64));
+            top = fmaxf(top, __shfl_xor(top, 32, 64));
+            const int e = top > 0.0f && top < INFINITY ? ilogbf(top) - 14 : 0;   // the largest to 2^14 .. 2^15
+            unit[t] = ldexpf(unit[t], e);
+#pragma unroll
+            for (int k = 0; k < KM; ++k)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[k][j] = ldexpf(v[k][j], -e);
+        }
+#pragma unroll
+        for (int k = 0; k < KM; ++k) {
+            half8v hi, lo;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {   // places 2 j, 2 j + 1 of a word: nibbles j, j + 4
+                const float f = v[k][(j & 1) * 4 + (j >> 1)];
+                hi[j] = (_Float16)f;
+                lo[j] = (_Float16)(f - (float)hi[j]);
+            }
+            qh[t][k] = hi;
+            if constexpr (kTwo) ql[t][k] = lo;
+        }
+    }
+
+    const size_t block = (size_t)bh * a.T;
+    const uint8_t *kc = static_cast<const uint8_t *>(a.codesK) + block * (D / 2), *vc = static_cast<const uint8_t *>(a.codesV) + block * (D / 2);
+    const uint32_t *kp = static_cast<const uint32_t *>(a.paramsK) + block * (D / a.group_k) + (size_t)(kg * (D / 4) / a.group_k) * a.T;
+    const uint32_t *vp = static_cast<const uint32_t *>(a.paramsV) + block * (D / a.group_v) + (size_t)(m * UC / a.group_v) * a.T;
+
+    float4v o[NR][UC] = {};
+    float top[NR], sum[NR];
+#pragma unroll
+    for (int t = 0; t < NR; ++t) { top[t] = kNone; sum[t] = 0.0f; }
+
+    Raw<D> next;
+    int tb = begin + wave * kStep;
+    if (tb < end) request<D>(next, kc, kp, vc, vp, tb, (int)a.T, m, kg);
+    for (; tb < end; tb += kStep * W) {
+        Raw<D> r = next;
+        if (tb + kStep * W < end) request<D>(next, kc, kp, vc, vp, tb + kStep * W, (int)a.T, m, kg);
+
+        half8v k8[2][KM];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const half2v ks = as_half2(low_halves(r.kp[u], r.kp[u])), km = as_half2(high_halves(r.kp[u], r.kp[u]));
+#pragma unroll
+            for (int k = 0; k < KM; ++k)
+                k8[u][k] = join(fma2(nibble_pair<0>(r.kc[u][k]), ks, km), fma2(nibble_pair<1>(r.kc[u][k]), ks, km),
+                                fma2(nibble_pair<2>(r.kc[u][k]), ks, km), fma2(nibble_pair<3>(r.kc[u][k]), ks, km));
+        }
+        float score[NR][8];
+#pragma unroll
+        for (int t = 0; t < NR; ++t)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                float4v c = {};
+#pragma unroll
+                for (int k = 0; k < KM; ++k) {
+                    c = mfma(k8[u][k], qh[t][k], c);
+                    if constexpr (kTwo) c = mfma(k8[u][k], ql[t][k], c);
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) score[t][4 * u + j] = c[j];
+            }
+        // tokens that some row does not see: out of its scores, and values that are no finite numbers out of the product - the
+        // rows that do see them get NaN
+        if (tb + kStep > s.all) {
+            bool any_bad = false;
+            half8v bad;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const half2v sm = as_half2(r.vp[j]);
+                const half2v ends = half2v{__builtin_elementwise_fma((_Float16)15.0f, sm[0], sm[1]), sm[1]};
+                const bool bj = not_finite(as_u32(ends));
+                any_bad |= bj;
+                bad[j] = bj ? (_Float16)1.0f : (_Float16)0.0f;
+                if (bj) r.vp[j] = 0;
+            }
+            const bool poisoned = __any(any_bad);
+#pragma unroll
+            for (int t = 0; t < NR; ++t) {
+                half8v seen;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const bool sees = tb + 8 * kg + j <= limit[t];
+                    if (!sees) score[t][j] = -INFINITY;
+                    seen[j] = sees ? (_Float16)1.0f : (_Float16)0.0f;
+                }
+                if (poisoned) {
+                    const float4v n = mfma(bad, seen, float4v{});
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int c = 0; c < UC; ++c) o[t][c][j] = n[j] > 0.0f ? NAN : o[t][c][j];
+                }
+            }
+        }
+        half8v ph[NR], pl[NR];
+#pragma unroll
+        for (int t = 0; t < NR; ++t) {
+            float best = score[t][0];
+#pragma unroll
+            for (int j = 1; j < 8; ++j) best = fmaxf(best, score[t][j]);
+            best *= unit[t];
+            if (__any(best > top[t] + kSlack)) {
+                best = fmaxf(best, __shfl_xor(best, 16, 64));
+                best = fmaxf(best, __shfl_xor(best, 32, 64));
+                best = fmaxf(best, top[t]);
+                const float fade = __builtin_amdgcn_exp2f(top[t] - best);
+                top[t] = best;
+                sum[t] *= fade;
+#pragma unroll
+                for (int c = 0; c < UC; ++c) o[t][c] *= fade;
+            }
+            const float base = kShift - top[t];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float p = __builtin_amdgcn_exp2f(fmaf(score[t][j], unit[t], base));
+                sum[t] += p;
+                ph[t][j] = (_Float16)p;
+                pl[t][j] = (_Float16)(p - (float)ph[t][j]);
+            }
+        }
+        half2v vs[4], vm[4];
+        uint32_t lo[4], hi[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            vs[j] = as_half2(low_halves(r.vp[2 * j], r.vp[2 * j + 1]));
+            vm[j] = as_half2(high_halves(r.vp[2 * j], r.vp[2 * j + 1]));
+            lo[j] = low_halves(r.vc[2 * j], r.vc[2 * j + 1]);
+            hi[j] = high_halves(r.vc[2 * j], r.vc[2 * j + 1]);
+        }
+        const auto channel = [&](auto c) {
+            constexpr int C = decltype(c)::value, N = C & 3;
+            const uint32_t(&w)[4] = C < 4 ? lo : hi;
+            const half8v v8 = join(fma2(nibble_pair<N>(w[0]), vs[0], vm[0]), fma2(nibble_pair<N>(w[1]), vs[1], vm[1]),
+                                   fma2(nibble_pair<N>(w[2]), vs[2], vm[2]), fma2(nibble_pair<N>(w[3]), vs[3], vm[3]));
+#pragma unroll
+            for (int t = 0; t < NR; ++t) {
+                o[t][C] = mfma(v8, ph[t], o[t][C]);
+                o[t][C] = mfma(v8, pl[t], o[t][C]);
+            }
+        };
+        channel(std::integral_constant<int, 0>{});
+        channel(std::integral_constant<int, 1>{});
+        channel(std::integral_constant<int, 2>{});
+        channel(std::integral_constant<int, 3>{});
+        if constexpr (UC == 8) {
+            channel(std::integral_constant<int, 4>{});
+            channel(std::integral_constant<int, 5>{});
+            channel(std::integral_constant<int, 6>{});
+            channel(std::integral_constant<int, 7>{});
+        }
+    }
+
+    // the waves' parts of a row tile, one tile after the other
+    __shared__ float part[W][16][D + 4], parts_top[W][16], parts_sum[W][16];
+#pragma unroll
+    for (int t = 0; t < NR; ++t) {
+        float l = sum[t];
+        l += __shfl_xor(l, 16, 64);
+        l += __shfl_xor(l, 32, 64);
+        if (t > 0) __syncthreads();
+        if (kg == 0) {
+            parts_top[wave][m] = top[t];
+            parts_sum[wave][m] = l;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int c = 0; c < UC; c += 4)
+                *reinterpret_cast<float4v *>(&part[wave][m][(4 * kg + j) * UC + c]) = float4v{o[t][c][j], o[t][c + 1][j], o[t][c + 2][j], o[t][c + 3][j]};
+        __syncthreads();
+        for (int e = threadIdx.x; e < 16 * D; e += 64 * W) {
+            const int n = e / D, ch = e - n * D, r = row0 + 16 * t + n;
+            if (r >= row_end) break;   // (rows ascend with e)
+            float best = kNone, all = 0.0f, value = 0.0f;
+#pragma unroll
+            for (int w = 0; w < W; ++w) best = fmaxf(best, parts_top[w][n]);
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                const float fade = __builtin_amdgcn_exp2f(parts_top[w][n] - best);
+                all = fmaf(parts_sum[w][n], fade, all);
+                value = fmaf(part[w][n][ch], fade, value);
+            }
+            if (ka.splits == 1) {
+                const int i = r / a.G, hq = h * a.G + r - i * a.G;
+                store_out(a, (int64_t)b * a.out_stride[0] + (int64_t)hq * a.out_stride[1] + (int64_t)i * a.out_stride[2] + ch,
+                          all == 0.0f ? 0.0f : value / all);
+            } else {
+                const size_t at = ((size_t)bh * ka.splits + split) * ka.rows + r;
+                ka.acc[at * D + ch] = value;
+                if (ch == 0) {
+                    ka.ml[2 * at] = best;
+                    ka.ml[2 * at + 1] = all;
+                }
+            }
+        }
+    }
+}
+
+// Joins the parts of the token axis: a wave per query row
+template <int D>
+__global__ __launch_bounds__(256) void q4_join_kernel(AttnKernelArgs ka)
+{
+    constexpr int CH = D / 64;
+    const Q4AttnArgs &a = ka.a;
+    const int lane = threadIdx.x & 63;
+    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (row >= (int64_t)a.B * a.Hkv * ka.rows) return;
+    const int bh = (int)(row / ka.rows), r = (int)(row - (int64_t)bh * ka.rows), b = bh / a.Hkv, h = bh - b * a.Hkv;
+    const size_t first = (size_t)bh * ka.splits * ka.rows + r;
+    float best = kNone, all = 0.0f, value[CH] = {};
+    for (int k = lane; k < ka.splits; k += 64) best = fmaxf(best, ka.ml[2 * (first + (size_t)k * ka.rows)]);
+#pragma unroll
+    for (int w = 32; w >= 1; w >>= 1) best = fmaxf(best, __shfl_xor(best, w, 64));
+    for (int k = 0; k < ka.splits; ++k) {
+        const size_t at = first + (size_t)k * ka.rows;
+        const float fade = __builtin_amdgcn_exp2f(ka.ml[2 * at] - best);
+        all = fmaf(ka.ml[2 * at + 1], fade, all);
+#pragma unroll
+        for (int c = 0; c < CH; ++c) value[c] = fmaf(ka.acc[at * D + lane * CH + c], fade, value[c]);
+    }
+    const int i = r / a.G, hq = h * a.G + r - i * a.G;
+    const int64_t at = (int64_t)b * a.out_stride[0] + (int64_t)hq * a.out_stride[1] + (int64_t)i * a.out_stride[2] + lane * CH;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) store_out(a, at + c, all == 0.0f ? 0.0f : value[c] / all);
+}
+
+constexpr int kWaves = 4;
+
+template <int D, int QMODE, int NR> hipError_t run(const AttnKernelArgs &ka)
+{
+    const int64_t groups = (int64_t)ka.a.B * ka.a.Hkv * ka.splits * ka.row_blocks;
+    hipLaunchKernelGGL((q4_stream_kernel<D, QMODE, NR, kWaves>), dim3((unsigned)groups), dim3(64 * kWaves), 0, ka.a.stream, ka);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || ka.splits == 1) return e;
+    const int64_t rows = (int64_t)ka.a.B * ka.a.Hkv * ka.rows;
+    hipLaunchKernelGGL((q4_join_kernel<D>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, ka.a.stream, ka);
+    return hipGetLastError();
+}
+template <int D, int QMODE> hipError_t run(const AttnKernelArgs &ka, int row_tiles)
+{
+    return row_tiles == 1 ? run<D, QMODE, 1>(ka) : run<D, QMODE, 2>(ka);
+}
+template <int D> hipError_t run(const AttnKernelArgs &ka, int row_tiles)
+{
+    switch (ka.a.q_dtype) {
+        case CSR_F32: return run<D, CSR_F32>(ka, row_tiles);
+        case CSR_F16: return run<D, CSR_F16>(ka, row_tiles);
+        default: return run<D, CSR_BF16>(ka, row_tiles);
+    }
+}
+
+}  // namespace
+
+void plan_q4_attn(const Q4AttnArgs &a, Q4AttnPlan *p)
+{
+    const int64_t rows = (int64_t)a.G * a.Tq, blocks = (int64_t)a.B * a.Hkv;
+    p->row_tiles = rows <= 16 ? 1 : 2;
+    p->row_blocks = (int32_t)((rows + 16 * p->row_tiles - 1) / (16 * p->row_tiles));
+    const int64_t groups = blocks * p->row_blocks, fill = 1024, by_tokens = (a.T + 255) / 256;
+    int64_t splits = groups ? (fill + groups - 1) / groups : 1;
+    if (splits > by_tokens) splits = by_tokens;
+    if (splits < 1) splits = 1;
+    p->splits = (int32_t)splits;
+    const size_t parts = (size_t)blocks * (size_t)rows * (size_t)splits;
+    p->off_ml = splits > 1 ? (parts * a.d * 4 + 255) / 256 * 256 : 0;
+    p->total_bytes = splits > 1 ? p->off_ml + (parts * 8 + 255) / 256 * 256 : 0;
+}
+
+hipError_t launch_q4_attn(const Q4AttnArgs &a, const Q4AttnPlan &p)
+{
+    AttnKernelArgs ka{a, p.splits, p.row_blocks, a.G * a.Tq, static_cast<float *>(a.workspace), nullptr};
+    ka.ml = reinterpret_cast<float *>(static_cast<char *>(a.workspace) + p.off_ml);
+    return a.d == 128 ? run<128>(ka, p.row_tiles) : run<64>(ka, p.row_tiles);
+}
+
+}  // namespace csr

@@ -4,7 +4,7 @@
 // ctypes structures and arguments, two torch.empty) they took about 25 us of host time each, so a decoding step was
 // bound by the interpreter.  Here the same marshalling is 1 to 2 us plus the launches.
 //
-// Three functions: encode, decode, reconstruct.  Each takes the arguments of the Python function of the same name by
+// encode, decode, reconstruct; q4_write, q4_read, q4_attn for the 4-bit cache.  Each takes the arguments of the Python function of the same name by
 // position and returns its result - or None for anything out of the ordinary (an argument that is not a GPU tensor, a
 // shape or type that does not fit, a status other than CSR_OK): the Python function then goes through its own checks,
 // which name the mistake.  Nothing has been launched in that case, except where the runtime itself reports an error.
@@ -31,6 +31,10 @@ struct Api {
     size_t (*decode_workspace)(const csr_decode_desc *);
     decltype(&csr_decode_attn) decode;
     decltype(&csr_reconstruct) reconstruct;
+    decltype(&csr_q4_write) q4_write;
+    decltype(&csr_q4_read) q4_read;
+    size_t (*q4_attn_workspace)(const csr_q4_attn_desc *);
+    decltype(&csr_q4_attn) q4_attn;
 } api;
 
 constexpr size_t kInvalid = (size_t)-1;
@@ -318,6 +322,183 @@ PyObject *reconstruct(PyObject *, PyObject *const *a, Py_ssize_t n)
     return output(a[3], made);
 }
 
+// ---- the 4-bit cache -------------------------------------------------------------------------------------------------
+// A GPU tensor of the current device, or nullptr: the calls below run on that device's current stream
+const Tensor *here(PyObject *o)
+{
+    const Tensor *t = gpu_tensor(o);
+    return t && t->get_device() == c10::hip::current_device() ? t : nullptr;
+}
+int q4_dtype(ScalarType t) { return t == ScalarType::BFloat16 ? CSR_BF16 : dtype_code(t); }
+
+// codes [B, Hkv, T, d / 2] and params [B, Hkv, d / group, T, 2] of a cache
+bool q4_cache(const Tensor *codes, const Tensor *params)
+{
+    if (!codes || !params || codes->scalar_type() != ScalarType::Byte || params->scalar_type() != ScalarType::Half || codes->dim() != 4 ||
+        params->dim() != 5 || !codes->is_contiguous() || !params->is_contiguous())
+        return false;
+    const int64_t d = 2 * codes->size(3), groups = params->size(2);
+    return groups > 0 && d % groups == 0 && d <= 128 && params->size(0) == codes->size(0) && params->size(1) == codes->size(1) &&
+           params->size(3) == codes->size(2) && params->size(4) == 2 && codes->size(0) <= INT32_MAX && codes->size(1) <= INT32_MAX;
+}
+bool q4_dense(const Tensor *t, at::IntArrayRef shape) { return t && t->sizes() == shape && q4_dtype(t->scalar_type()) >= 0 && t->stride(-1) == 1; }
+// An int32 tensor [B], or None
+bool q4_lens(PyObject *o, int64_t B, const int32_t **p)
+{
+    *p = nullptr;
+    if (o == Py_None) return true;
+    const Tensor *t = here(o);
+    if (!t || t->scalar_type() != ScalarType::Int || t->numel() != B || !t->is_contiguous()) return false;
+    *p = static_cast<const int32_t *>(t->data_ptr());
+    return true;
+}
+csr_q4_rows_desc q4_rows_desc(const Tensor *x, const Tensor *out, const Tensor &codes, const Tensor &params, int64_t n, int64_t pos0, ScalarType dt)
+{
+    csr_q4_rows_desc e{};
+    e.B = (int32_t)codes.size(0); e.Hkv = (int32_t)codes.size(1); e.n = n; e.T = codes.size(2);
+    e.d = (int32_t)(2 * codes.size(3)); e.group = (int32_t)(e.d / params.size(2)); e.pos0 = pos0;
+    e.out_dtype = q4_dtype(dt);
+    if (x) { e.x_dtype = q4_dtype(x->scalar_type()); e.x_stride_b = x->stride(0); e.x_stride_h = x->stride(1); e.x_stride_t = x->stride(2); }
+    if (out) { e.out_stride_b = out->stride(0); e.out_stride_h = out->stride(1); e.out_stride_t = out->stride(2); }
+    return e;
+}
+
+// (K, codesK, paramsK, V, codesV, paramsV, pos0, pos, counts, values, outK, outV) -> (None | out | (outK, outV),)
+PyObject *q4_write(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    if (n_args != 12) CSR_PUNT();
+    const int sides = a[3] == Py_None ? 1 : 2;
+    const Tensor *x[2] = {}, *codes[2] = {}, *params[2] = {}, *given[2] = {};
+    for (int k = 0; k < 2; ++k) {
+        if (k >= sides) {
+            if (a[4] != Py_None || a[5] != Py_None || a[11] != Py_None) CSR_PUNT();
+            break;
+        }
+        x[k] = here(a[3 * k]); codes[k] = here(a[3 * k + 1]); params[k] = here(a[3 * k + 2]);
+        if (!x[k] || x[k]->dim() != 4 || !q4_cache(codes[k], params[k]) || codes[k]->sizes() != codes[0]->sizes()) CSR_PUNT();
+        if (a[10 + k] != Py_None && !(given[k] = here(a[10 + k]))) CSR_PUNT();
+    }
+    if (sides == 2 && (given[0] == nullptr) != (given[1] == nullptr)) CSR_PUNT();
+    const int64_t B = codes[0]->size(0), n = x[0]->size(2), shape4[4] = {B, codes[0]->size(1), n, 2 * codes[0]->size(3)};
+    const at::IntArrayRef shape(shape4, 4);
+    const ScalarType dt = x[0]->scalar_type();
+    for (int k = 0; k < sides; ++k)
+        if (!q4_dense(x[k], shape) || x[k]->scalar_type() != dt || (given[k] && (!q4_dense(given[k], shape) || given[k]->scalar_type() != dt))) CSR_PUNT();
+    int64_t pos0;
+    const int32_t *pos, *counts;
+    if (!int_arg(a[6], &pos0) || !q4_lens(a[7], B, &pos) || !q4_lens(a[8], B, &counts)) CSR_PUNT();
+    const int values = PyObject_IsTrue(a[9]);
+    if (values < 0) { PyErr_Clear(); CSR_PUNT(); }
+    const bool outs = values || given[0];
+    Tensor made[2];
+    csr_status st;
+    {
+        Unlocked unlocked;
+        csr_q4_rows_desc e[2];
+        const Tensor *out[2] = {};
+        for (int k = 0; k < sides; ++k) {
+            if (outs && !given[k]) made[k] = fresh(shape, dt, *x[k]);
+            if (outs) out[k] = given[k] ? given[k] : &made[k];
+            e[k] = q4_rows_desc(x[k], out[k], *codes[k], *params[k], n, pos0, dt);
+        }
+        const auto ptr = [](const Tensor *t) { return t ? t->data_ptr() : nullptr; };
+        st = api.q4_write(&e[0], ptr(x[0]), ptr(codes[0]), ptr(params[0]), ptr(out[0]), sides == 2 ? &e[1] : nullptr, ptr(x[1]), ptr(codes[1]),
+                          ptr(params[1]), ptr(out[1]), pos, counts, stream());
+    }
+    if (st != CSR_OK) CSR_PUNT();
+    PyObject *result;
+    if (!outs) {
+        Py_INCREF(Py_None);
+        result = Py_None;
+    } else if (sides == 1) {
+        result = output(a[10], made[0]);
+    } else {
+        result = PyTuple_New(2);
+        for (int k = 0; k < 2 && result; ++k) {
+            PyObject *o = output(a[10 + k], made[k]);
+            if (o) PyTuple_SET_ITEM(result, k, o);
+            else Py_CLEAR(result);
+        }
+    }
+    PyObject *done = result ? PyTuple_New(1) : nullptr;
+    if (done) PyTuple_SET_ITEM(done, 0, result);
+    else Py_XDECREF(result);
+    return done;
+}
+
+// (codes, params, n, pos0, pos, counts, out, out_dtype) -> out
+PyObject *q4_read(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    if (n_args != 8) CSR_PUNT();
+    const Tensor *codes = here(a[0]), *params = here(a[1]), *given = nullptr;
+    if (!q4_cache(codes, params) || (a[6] != Py_None && !(given = here(a[6])))) CSR_PUNT();
+    const int64_t B = codes->size(0), T = codes->size(2);
+    int64_t pos0, n;
+    const int32_t *pos, *counts;
+    ScalarType dt;
+    if (!int_arg(a[3], &pos0) || !q4_lens(a[4], B, &pos) || !q4_lens(a[5], B, &counts) ||
+        !dtype_arg(a[7], given ? given->scalar_type() : ScalarType::Half, &dt) || q4_dtype(dt) < 0)
+        CSR_PUNT();
+    if (a[2] == Py_None) n = given && given->dim() == 4 ? given->size(2) : T - (pos0 > 0 ? pos0 : 0) > 0 ? T - (pos0 > 0 ? pos0 : 0) : 0;
+    else if (!int_arg(a[2], &n) || n < 0) CSR_PUNT();
+    const int64_t shape4[4] = {B, codes->size(1), n, 2 * codes->size(3)};
+    const at::IntArrayRef shape(shape4, 4);
+    if (given && (!q4_dense(given, shape) || given->scalar_type() != dt)) CSR_PUNT();
+    Tensor made;
+    csr_status st;
+    {
+        Unlocked unlocked;
+        if (!given) made = fresh(shape, dt, *codes);
+        const Tensor &out = given ? *given : made;
+        const csr_q4_rows_desc e = q4_rows_desc(nullptr, &out, *codes, *params, n, pos0, dt);
+        st = api.q4_read(&e, codes->data_ptr(), params->data_ptr(), out.data_ptr(), pos, counts, stream());
+    }
+    if (st != CSR_OK) CSR_PUNT();
+    return output(a[6], made);
+}
+
+// (q, codesK, paramsK, codesV, paramsV, scale, seq_lens, q_lens, causal, out, out_dtype, workspace) -> out
+PyObject *q4_attn(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    if (n_args != 12) CSR_PUNT();
+    const Tensor *q = here(a[0]), *cK = here(a[1]), *pK = here(a[2]), *cV = here(a[3]), *pV = here(a[4]), *given = nullptr, *workspace = nullptr;
+    if (!q || !q4_cache(cK, pK) || !q4_cache(cV, pV) || cK->sizes() != cV->sizes() || (q->dim() != 3 && q->dim() != 4)) CSR_PUNT();
+    if ((a[9] != Py_None && !(given = here(a[9]))) || (a[11] != Py_None && !(workspace = here(a[11])))) CSR_PUNT();
+    const bool many = q->dim() == 4;
+    const int64_t B = cK->size(0), Hq = q->size(1), Tq = many ? q->size(2) : 1, d = 2 * cK->size(3);
+    csr_q4_attn_desc e{};
+    const int32_t *lens, *q_lens;
+    ScalarType ot;
+    if (q->size(0) != B || q->size(-1) != d || q->stride(-1) != 1 || Hq > INT32_MAX || Tq > INT32_MAX || q4_dtype(q->scalar_type()) < 0 ||
+        !float_arg(a[5], &e.scale) || !q4_lens(a[6], B, &lens) || !q4_lens(a[7], B, &q_lens) ||
+        !dtype_arg(a[10], given ? given->scalar_type() : q->scalar_type(), &ot) || q4_dtype(ot) < 0)
+        CSR_PUNT();
+    if (given && (!q4_dense(given, q->sizes()) || given->scalar_type() != ot)) CSR_PUNT();
+    const int causal = PyObject_IsTrue(a[8]);
+    if (causal < 0) { PyErr_Clear(); CSR_PUNT(); }
+    e.B = (int32_t)B; e.Hq = (int32_t)Hq; e.Hkv = (int32_t)cK->size(1); e.Tq = (int32_t)Tq; e.T = cK->size(2); e.d = (int32_t)d;
+    e.group_k = (int32_t)(d / pK->size(2)); e.group_v = (int32_t)(d / pV->size(2));
+    e.q_dtype = q4_dtype(q->scalar_type()); e.out_dtype = q4_dtype(ot);
+    e.q_stride_b = q->stride(0); e.q_stride_h = q->stride(1); e.q_stride_t = many ? q->stride(2) : 0;
+    e.flags = causal ? 0u : CSR_FLAG_NOT_CAUSAL;
+    Tensor made;
+    csr_status st = CSR_ERR_WORKSPACE;
+    {
+        Unlocked unlocked;
+        if (!given) made = fresh(q->sizes(), ot, *q);
+        const Tensor &out = given ? *given : made;
+        e.out_stride_b = out.stride(0); e.out_stride_h = out.stride(1); e.out_stride_t = many ? out.stride(2) : 0;
+        const size_t need = api.q4_attn_workspace(&e);
+        if (need != kInvalid) {
+            const Workspace ws(workspace, need);
+            st = api.q4_attn(&e, q->data_ptr(), cK->data_ptr(), pK->data_ptr(), cV->data_ptr(), pV->data_ptr(), lens, q_lens, out.data_ptr(),
+                             ws.ptr, ws.bytes, stream());
+        }
+    }
+    if (st != CSR_OK) CSR_PUNT();
+    return output(a[9], made);
+}
+
 // C++ exceptions of PyTorch (an allocation that fails) must not cross into the interpreter: the Python path meets the
 // same condition and reports it in PyTorch's own way.
 template <PyObject *(*F)(PyObject *, PyObject *const *, Py_ssize_t)>
@@ -330,15 +511,16 @@ PyObject *guarded(PyObject *self, PyObject *const *a, Py_ssize_t n)
     }
 }
 
-// bind(encode_workspace_bytes, encode, decode_workspace_bytes, decode_attn, reconstruct): addresses of the entry points
+// bind(encode_workspace_bytes, encode, decode_workspace_bytes, decode_attn, reconstruct, q4_write, q4_read, q4_attn_workspace_bytes,
+// q4_attn): addresses of the entry points
 PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
-    void *p[5];
-    if (n != 5) {
-        PyErr_SetString(PyExc_TypeError, "bind takes five addresses");
+    void *p[9];
+    if (n != 9) {
+        PyErr_SetString(PyExc_TypeError, "bind takes nine addresses");
         return nullptr;
     }
-    for (int k = 0; k < 5; ++k) {
+    for (int k = 0; k < 9; ++k) {
         p[k] = PyLong_AsVoidPtr(a[k]);
         if (!p[k]) {
             if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "bind: null address");
@@ -350,6 +532,10 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
     api.decode_workspace = reinterpret_cast<decltype(api.decode_workspace)>(p[2]);
     api.decode = reinterpret_cast<decltype(api.decode)>(p[3]);
     api.reconstruct = reinterpret_cast<decltype(api.reconstruct)>(p[4]);
+    api.q4_write = reinterpret_cast<decltype(api.q4_write)>(p[5]);
+    api.q4_read = reinterpret_cast<decltype(api.q4_read)>(p[6]);
+    api.q4_attn_workspace = reinterpret_cast<decltype(api.q4_attn_workspace)>(p[7]);
+    api.q4_attn = reinterpret_cast<decltype(api.q4_attn)>(p[8]);
     Py_RETURN_NONE;
 }
 
@@ -358,6 +544,9 @@ PyMethodDef methods[] = {{"bind", CSR_FN(bind), METH_FASTCALL, nullptr},
                          {"encode", CSR_FN(guarded<encode>), METH_FASTCALL, nullptr},
                          {"decode", CSR_FN(guarded<decode>), METH_FASTCALL, nullptr},
                          {"reconstruct", CSR_FN(guarded<reconstruct>), METH_FASTCALL, nullptr},
+                         {"q4_write", CSR_FN(guarded<q4_write>), METH_FASTCALL, nullptr},
+                         {"q4_read", CSR_FN(guarded<q4_read>), METH_FASTCALL, nullptr},
+                         {"q4_attn", CSR_FN(guarded<q4_attn>), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_csr_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
