@@ -96,42 +96,66 @@ template <int D> struct Raw {
     uint32_t kc[2][D / 32], kp[2], vc[8], vp[8];
 };
 
-template <int D>
-__device__ __forceinline__ void request(Raw<D> &r, const uint8_t *kc, const uint32_t *kp, const uint8_t *vc, const uint32_t *vp, int tb, int T, int m, int kg)
+// Where a lane's codes and parameters lie, as bytes behind those of a wave's first token
+struct Lane {
+    uint32_t kc, kp, vc, vp;
+};
+
+typedef uint4v uint4a __attribute__((aligned(4)));
+
+// WHOLE: all 32 tokens are rows of the cache.  Else rows behind the last one are requested as the last one.
+template <int D, bool WHOLE>
+__device__ __forceinline__ void request(Raw<D> &r, const Q4AttnArgs &a, size_t block, const Lane &at, int tb, int m, int kg)
 {
-    const int last = T - 1;
+    const uint8_t *kc = static_cast<const uint8_t *>(a.codesK) + (block + tb) * (D / 2), *vc = static_cast<const uint8_t *>(a.codesV) + (block + tb) * (D / 2);
+    const uint8_t *kp = static_cast<const uint8_t *>(a.paramsK) + (block * (D / a.group_k) + tb) * 4;
+    const uint8_t *vp = static_cast<const uint8_t *>(a.paramsV) + (block * (D / a.group_v) + tb) * 4;
+    const int last = (int)a.T - 1 - tb;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-        const int t = min(tb + 8 * (m >> 2) + (m & 3) + 4 * u, last);
+        const int mine = 8 * (m >> 2) + (m & 3) + 4 * u, back = WHOLE ? 0 : max(0, mine - last);
+        const uint32_t c = at.kc + 4 * u * (D / 2) - back * (D / 2);
         if constexpr (D == 128) {
-            const uint4v w = *reinterpret_cast<const uint4v *>(kc + (size_t)t * 64 + kg * 16);
+            const uint4v w = *reinterpret_cast<const uint4v *>(kc + c);
 #pragma unroll
             for (int k = 0; k < 4; ++k) r.kc[u][k] = w[k];
         } else {
-            const uint2v w = *reinterpret_cast<const uint2v *>(kc + (size_t)t * 32 + kg * 8);
+            const uint2v w = *reinterpret_cast<const uint2v *>(kc + c);
             r.kc[u][0] = w[0];
             r.kc[u][1] = w[1];
         }
-        r.kp[u] = kp[t];
+        r.kp[u] = *reinterpret_cast<const uint32_t *>(kp + (at.kp + 16 * u - back * 4));
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        const int t = min(tb + 8 * kg + j, last);
-        if constexpr (D == 128) r.vc[j] = *reinterpret_cast<const uint32_t *>(vc + (size_t)t * 64 + m * 4);
-        else r.vc[j] = *reinterpret_cast<const uint16_t *>(vc + (size_t)t * 32 + m * 2);
-        r.vp[j] = vp[t];
+        const int back = WHOLE ? 0 : max(0, 8 * kg + j - last);
+        const uint32_t c = at.vc + j * (D / 2) - back * (D / 2);
+        if constexpr (D == 128) r.vc[j] = *reinterpret_cast<const uint32_t *>(vc + c);
+        else r.vc[j] = *reinterpret_cast<const uint16_t *>(vc + c);
+        if constexpr (!WHOLE) r.vp[j] = *reinterpret_cast<const uint32_t *>(vp + (at.vp + 4 * j - back * 4));
     }
+    if constexpr (WHOLE) {
+        const uint4v w0 = *reinterpret_cast<const uint4a *>(vp + at.vp), w1 = *reinterpret_cast<const uint4a *>(vp + (at.vp + 16));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { r.vp[j] = w0[j]; r.vp[4 + j] = w1[j]; }
+    }
+}
+template <int D>
+__device__ __forceinline__ void request(Raw<D> &r, const Q4AttnArgs &a, size_t block, const Lane &at, int tb, int m, int kg)
+{
+    if (tb + kStep <= (int)a.T) request<D, true>(r, a, block, at, tb, m, kg);
+    else request<D, false>(r, a, block, at, tb, m, kg);
 }
 
 // QMODE: csr_dtype of q.  NR: tiles of 16 query rows.  W: waves.
 template <int D, int QMODE, int NR, int W>
-__global__ __launch_bounds__(64 * W) void q4_stream_kernel(AttnKernelArgs ka)
+__global__ __launch_bounds__(64 * W, NR == 1 ? 3 : 2) void q4_stream_kernel(AttnKernelArgs ka)
 {
     constexpr int KM = D / 32;   // matrix instructions along a key's channels
     constexpr int UC = D / 16;   // channels of a lane's values
     constexpr bool kTwo = QMODE == CSR_F32;
     const Q4AttnArgs &a = ka.a;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, kg = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, kg = lane >> 4;
     int x = blockIdx.x;
     const int rb = x % ka.row_blocks;
     x /= ka.row_blocks;
@@ -184,9 +208,9 @@ __global__ __launch_bounds__(64 * W) void q4_stream_kernel(AttnKernelArgs ka)
     }
 
     const size_t block = (size_t)bh * a.T;
-    const uint8_t *kc = static_cast<const uint8_t *>(a.codesK) + block * (D / 2), *vc = static_cast<const uint8_t *>(a.codesV) + block * (D / 2);
-    const uint32_t *kp = static_cast<const uint32_t *>(a.paramsK) + block * (D / a.group_k) + (size_t)(kg * (D / 4) / a.group_k) * a.T;
-    const uint32_t *vp = static_cast<const uint32_t *>(a.paramsV) + block * (D / a.group_v) + (size_t)(m * UC / a.group_v) * a.T;
+    const uint32_t T = (uint32_t)a.T, token = 8 * (m >> 2) + (m & 3);
+    const Lane at{token * (D / 2) + kg * (D / 8), ((uint32_t)(kg * (D / 4) / a.group_k) * T + token) * 4,
+                  (uint32_t)(8 * kg * (D / 2) + m * (D / 32)), ((uint32_t)(m * UC / a.group_v) * T + 8 * kg) * 4};
 
     float4v o[NR][UC] = {};
     float top[NR], sum[NR];
@@ -195,10 +219,10 @@ __global__ __launch_bounds__(64 * W) void q4_stream_kernel(AttnKernelArgs ka)
 
     Raw<D> next;
     int tb = begin + wave * kStep;
-    if (tb < end) request<D>(next, kc, kp, vc, vp, tb, (int)a.T, m, kg);
+    if (tb < end) request<D>(next, a, block, at, tb, m, kg);
     for (; tb < end; tb += kStep * W) {
         Raw<D> r = next;
-        if (tb + kStep * W < end) request<D>(next, kc, kp, vc, vp, tb + kStep * W, (int)a.T, m, kg);
+        if (tb + kStep * W < end) request<D>(next, a, block, at, tb + kStep * W, m, kg);
 
         half8v k8[2][KM];
 #pragma unroll
@@ -279,7 +303,7 @@ __global__ __launch_bounds__(64 * W) void q4_stream_kernel(AttnKernelArgs ka)
                 const float p = __builtin_amdgcn_exp2f(fmaf(score[t][j], unit[t], base));
                 sum[t] += p;
                 ph[t][j] = (_Float16)p;
-                pl[t][j] = (_Float16)(p - (float)ph[t][j]);
+                pl[t][j] = (_Float16)fmaf((float)ph[t][j], -1.0f, p);
             }
         }
         half2v vs[4], vm[4];

@@ -20,15 +20,24 @@ __device__ __forceinline__ uint32_t as_u32(half2v v) { return __builtin_bit_cast
 __device__ __forceinline__ half2v fma2(half2v a, half2v b, half2v c) { return __builtin_elementwise_fma(a, b, c); }
 __device__ __forceinline__ half2v splat2(float v) { return half2v{(_Float16)v, (_Float16)v}; }
 
+// (v & mask) | bits in one instruction: the mask in a scalar register, the bits in a vector one.  The compiler makes two of it,
+// with a literal each.
+__device__ __forceinline__ uint32_t and_or(uint32_t v, uint32_t mask, uint32_t bits)
+{
+    uint32_t r;
+    asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(r) : "v"(v), "s"(mask), "v"(bits));
+    return r;
+}
+
 // Nibbles K and K + 4 of w as fp16 whole numbers.  A nibble in the lowest bits of an fp16 with the exponent of 1024 reads as
 // 1024 + code, four bits higher as 1024 + 16 code; either way one packed operation leaves the code, exactly.
 template <int K> __device__ __forceinline__ half2v nibble_pair(uint32_t w)
 {
     const uint32_t v = K >= 2 ? w >> 8 : w;
     if constexpr (K % 2 == 0)
-        return as_half2((v & 0x000f000fu) | 0x64006400u) - splat2(1024.0f);
+        return as_half2(and_or(v, 0x000f000fu, 0x64006400u)) - splat2(1024.0f);
     else
-        return fma2(as_half2((v & 0x00f000f0u) | 0x64006400u), splat2(0.0625f), splat2(-64.0f));
+        return fma2(as_half2(and_or(v, 0x00f000f0u, 0x64006400u)), splat2(0.0625f), splat2(-64.0f));
 }
 
 // The low (high) halves of two words side by side
