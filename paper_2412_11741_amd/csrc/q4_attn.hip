@@ -37,9 +37,25 @@ __device__ __forceinline__ half8v join(half2v a, half2v b, half2v c, half2v d)
     return half8v{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
+// p less the fp16 in the low (high) half of a word, exactly
+__device__ __forceinline__ float less_low(float p, uint32_t h)
+{
+    float r;
+    asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(r) : "v"(h), "v"(p));
+    return r;
+}
+__device__ __forceinline__ float less_high(float p, uint32_t h)
+{
+    float r;
+    asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(r) : "v"(h), "v"(p));
+    return r;
+}
+
 struct AttnKernelArgs {
     Q4AttnArgs a;
     int32_t splits, row_blocks, rows;
+    int32_t log_group_k, log_group_v;
+    FastDiv by_splits, by_group;
     float *acc, *ml;
 };
 
@@ -47,48 +63,53 @@ struct AttnKernelArgs {
 struct Sight {
     int len, qn, end, all;
 };
-__device__ __forceinline__ Sight sight_of(const Q4AttnArgs &a, int b, int row0, int row_end)
+__device__ __forceinline__ Sight sight_of(const AttnKernelArgs &ka, int len, int qn, int row0, int row_end)
 {
     Sight s;
-    s.len = (int)a.T;
-    if (a.seq_lens) s.len = max(0, min(a.seq_lens[b], (int)a.T));
-    s.qn = a.q_lens ? max(0, min(a.q_lens[b], a.Tq)) : a.Tq;
-    const int first = row0 / a.G, last = min((row_end - 1) / a.G, s.qn - 1);
+    s.len = max(0, min(len, (int)ka.a.T));
+    s.qn = max(0, min(qn, ka.a.Tq));
+    const int first = quotient(row0, ka.by_group), last = quotient(row_end - 1, ka.by_group);
     if (first >= s.qn) { s.end = s.all = 0; return s; }
-    s.end = a.causal ? max(0, s.len - s.qn + last + 1) : s.len;
-    s.all = (row_end - 1) / a.G >= s.qn ? 0 : a.causal ? max(0, s.len - s.qn + first + 1) : s.len;
+    s.end = ka.a.causal ? max(0, s.len - s.qn + min(last, s.qn - 1) + 1) : s.len;
+    s.all = last >= s.qn ? 0 : ka.a.causal ? max(0, s.len - s.qn + first + 1) : s.len;
     return s;
 }
-// The last token that query row r sees, -1 for none
-__device__ __forceinline__ int limit_of(const Q4AttnArgs &a, const Sight &s, int r, int rows)
+// The last token that query token i sees, -1 for none
+__device__ __forceinline__ int limit_of(const AttnKernelArgs &ka, const Sight &s, int i)
 {
-    const int i = r / a.G;
-    if (r >= rows || i >= s.qn) return -1;
-    return a.causal ? s.len - s.qn + i : s.len - 1;
+    if (i >= s.qn) return -1;
+    return ka.a.causal ? s.len - s.qn + i : s.len - 1;
 }
 
-__device__ __forceinline__ void store_out(const Q4AttnArgs &a, int64_t at, float v)
+// Four neighbouring channels of the output
+__device__ __forceinline__ void store_out4(const Q4AttnArgs &a, int64_t at, float4v v)
 {
-    if (a.out_dtype == CSR_F32) static_cast<float *>(a.out)[at] = v;
-    else if (a.out_dtype == CSR_F16) static_cast<_Float16 *>(a.out)[at] = (_Float16)v;
-    else static_cast<uint16_t *>(a.out)[at] = float_to_bf16(v);
-}
-
-// Eight channels of a query row as floats
-__device__ __forceinline__ void load_q8(const Q4AttnArgs &a, int64_t at, float (&v)[8])
-{
-    if (a.q_dtype == CSR_F32) {
-        const float4v *f = reinterpret_cast<const float4v *>(static_cast<const float *>(a.q) + at);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = f[k / 4][k % 4];
+    if (a.out_dtype == CSR_F32) {
+        *reinterpret_cast<float4v *>(static_cast<float *>(a.out) + at) = v;
+    } else if (a.out_dtype == CSR_F16) {
+        *reinterpret_cast<uint2v *>(static_cast<_Float16 *>(a.out) + at) =
+            uint2v{as_u32(half2v{(_Float16)v[0], (_Float16)v[1]}), as_u32(half2v{(_Float16)v[2], (_Float16)v[3]})};
     } else {
-        const uint4v w = *reinterpret_cast<const uint4v *>(static_cast<const uint16_t *>(a.q) + at);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            v[2 * k] = a.q_dtype == CSR_F16 ? (float)as_half2(w[k])[0] : __uint_as_float(w[k] << 16);
-            v[2 * k + 1] = a.q_dtype == CSR_F16 ? (float)as_half2(w[k])[1] : __uint_as_float(w[k] & 0xffff0000u);
-        }
+        *reinterpret_cast<uint2v *>(static_cast<uint16_t *>(a.out) + at) =
+            uint2v{(uint32_t)float_to_bf16(v[0]) | (uint32_t)float_to_bf16(v[1]) << 16, (uint32_t)float_to_bf16(v[2]) | (uint32_t)float_to_bf16(v[3]) << 16};
     }
+}
+
+// Eight channels of a query row, as they are stored
+template <int QMODE> struct Stored8 {
+    uint4v w[QMODE == CSR_F32 ? 2 : 1];
+};
+template <int QMODE> __device__ __forceinline__ void load_q8(Stored8<QMODE> &s, const void *q, int64_t at)
+{
+    const uint4v *p = reinterpret_cast<const uint4v *>(static_cast<const uint8_t *>(q) + at * (QMODE == CSR_F32 ? 4 : 2));
+    s.w[0] = p[0];
+    if constexpr (QMODE == CSR_F32) s.w[1] = p[1];
+}
+template <int QMODE> __device__ __forceinline__ float channel_of(const Stored8<QMODE> &s, int k)
+{
+    if constexpr (QMODE == CSR_F32) return __uint_as_float(s.w[k / 4][k % 4]);
+    else if constexpr (QMODE == CSR_F16) return (float)as_half2(s.w[0][k / 2])[k % 2];
+    else return __uint_as_float(k % 2 ? s.w[0][k / 2] & 0xffff0000u : s.w[0][k / 2] << 16);
 }
 
 // The codes and parameters of a wave's 32 tokens, as requested
@@ -96,7 +117,12 @@ template <int D> struct Raw {
     uint32_t kc[2][D / 32], kp[2], vc[8], vp[8];
 };
 
-// Where a lane's codes and parameters lie, as bytes behind those of a wave's first token
+// A (sequence, KV head) block of the caches, and where a lane's codes and parameters lie, as bytes behind those of a wave's first
+// token
+struct Base {
+    const uint8_t *kc, *kp, *vc, *vp;
+    int T;
+};
 struct Lane {
     uint32_t kc, kp, vc, vp;
 };
@@ -105,12 +131,11 @@ typedef uint4v uint4a __attribute__((aligned(4)));
 
 // WHOLE: all 32 tokens are rows of the cache.  Else rows behind the last one are requested as the last one.
 template <int D, bool WHOLE>
-__device__ __forceinline__ void request(Raw<D> &r, const Q4AttnArgs &a, size_t block, const Lane &at, int tb, int m, int kg)
+__device__ __forceinline__ void request(Raw<D> &r, const Base &base, const Lane &at, int tb, int m, int kg)
 {
-    const uint8_t *kc = static_cast<const uint8_t *>(a.codesK) + (block + tb) * (D / 2), *vc = static_cast<const uint8_t *>(a.codesV) + (block + tb) * (D / 2);
-    const uint8_t *kp = static_cast<const uint8_t *>(a.paramsK) + (block * (D / a.group_k) + tb) * 4;
-    const uint8_t *vp = static_cast<const uint8_t *>(a.paramsV) + (block * (D / a.group_v) + tb) * 4;
-    const int last = (int)a.T - 1 - tb;
+    const uint8_t *kc = base.kc + (uint32_t)tb * (D / 2), *vc = base.vc + (uint32_t)tb * (D / 2);
+    const uint8_t *kp = base.kp + (uint32_t)tb * 4, *vp = base.vp + (uint32_t)tb * 4;
+    const int last = base.T - 1 - tb;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
         const int mine = 8 * (m >> 2) + (m & 3) + 4 * u, back = WHOLE ? 0 : max(0, mine - last);
@@ -141,29 +166,49 @@ __device__ __forceinline__ void request(Raw<D> &r, const Q4AttnArgs &a, size_t b
     }
 }
 template <int D>
-__device__ __forceinline__ void request(Raw<D> &r, const Q4AttnArgs &a, size_t block, const Lane &at, int tb, int m, int kg)
+__device__ __forceinline__ void request(Raw<D> &r, const Base &base, const Lane &at, int tb, int m, int kg)
 {
-    if (tb + kStep <= (int)a.T) request<D, true>(r, a, block, at, tb, m, kg);
-    else request<D, false>(r, a, block, at, tb, m, kg);
+    if (tb + kStep <= base.T) request<D, true>(r, base, at, tb, m, kg);
+    else request<D, false>(r, base, at, tb, m, kg);
 }
 
 // QMODE: csr_dtype of q.  NR: tiles of 16 query rows.  W: waves.
 template <int D, int QMODE, int NR, int W>
-__global__ __launch_bounds__(64 * W, NR == 1 ? 3 : 2) void q4_stream_kernel(AttnKernelArgs ka)
+__global__ __launch_bounds__(64 * W, NR == 1 && QMODE != CSR_F32 ? 3 : 2) void q4_stream_kernel(AttnKernelArgs ka)
 {
     constexpr int KM = D / 32;   // matrix instructions along a key's channels
     constexpr int UC = D / 16;   // channels of a lane's values
     constexpr bool kTwo = QMODE == CSR_F32;
     const Q4AttnArgs &a = ka.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, kg = lane >> 4;
-    int x = blockIdx.x;
-    const int rb = x % ka.row_blocks;
-    x /= ka.row_blocks;
-    const int split = x % ka.splits, bh = x / ka.splits, b = bh / a.Hkv, h = bh - b * a.Hkv;
+    const int b = blockIdx.z, h = blockIdx.y, bh = b * a.Hkv + h;
+    const int rb = quotient(blockIdx.x, ka.by_splits), split = blockIdx.x - rb * ka.splits;
     const int row0 = rb * 16 * NR, row_end = min(row0 + 16 * NR, ka.rows);
-    const Sight s = sight_of(a, b, row0, row_end);
-    const int per = ((s.end + ka.splits - 1) / ka.splits + kStep * W - 1) / (kStep * W) * (kStep * W);
-    const int begin = min(split * per, s.end), end = min(begin + per, s.end);
+    const int len = a.seq_lens ? a.seq_lens[b] : (int)a.T, qn = a.q_lens ? a.q_lens[b] : a.Tq;
+
+    Stored8<QMODE> stored[NR][KM];
+    int query[NR];
+#pragma unroll
+    for (int t = 0; t < NR; ++t) {
+        const int r = min(row0 + 16 * t + m, ka.rows - 1), i = quotient(r, ka.by_group);
+        query[t] = row0 + 16 * t + m < ka.rows ? i : a.Tq;
+        const int64_t from = (int64_t)b * a.q_stride[0] + (int64_t)(h * a.G + r - i * a.G) * a.q_stride[1] + (int64_t)i * a.q_stride[2] + kg * (D / 4);
+#pragma unroll
+        for (int k = 0; k < KM; ++k) load_q8<QMODE>(stored[t][k], a.q, from + 8 * k);
+    }
+
+    const Sight s = sight_of(ka, len, qn, row0, row_end);
+    const uint32_t per = (quotient(s.end + ka.splits - 1, ka.by_splits) + kStep * W - 1) / (kStep * W) * (kStep * W);
+    const int begin = min((int)(split * per), s.end), end = min(begin + (int)per, s.end);
+    const size_t block = (size_t)bh * a.T;
+    const Base cache{static_cast<const uint8_t *>(a.codesK) + block * (D / 2), static_cast<const uint8_t *>(a.paramsK) + (block * D >> ka.log_group_k) * 4,
+                     static_cast<const uint8_t *>(a.codesV) + block * (D / 2), static_cast<const uint8_t *>(a.paramsV) + (block * D >> ka.log_group_v) * 4, (int)a.T};
+    const uint32_t T = (uint32_t)a.T, token = 8 * (m >> 2) + (m & 3);
+    const Lane at{token * (D / 2) + kg * (D / 8), ((uint32_t)(kg * (D / 4)) >> ka.log_group_k) * T * 4 + token * 4,
+                  (uint32_t)(8 * kg * (D / 2) + m * (D / 32)), ((uint32_t)(m * UC) >> ka.log_group_v) * T * 4 + 32 * kg};
+    Raw<D> even, odd;
+    int tb = begin + wave * kStep;
+    if (tb < end) request<D>(even, cache, at, tb, m, kg);
 
     // the queries: fp16, and what that lacks; in units that leave no loss to bf16
     half8v qh[NR][KM], ql[kTwo ? NR : 1][KM];
@@ -171,34 +216,27 @@ __global__ __launch_bounds__(64 * W, NR == 1 ? 3 : 2) void q4_stream_kernel(Attn
     int limit[NR];
 #pragma unroll
     for (int t = 0; t < NR; ++t) {
-        const int r = row0 + 16 * t + m;
-        limit[t] = limit_of(a, s, r, ka.rows);
+        limit[t] = limit_of(ka, s, query[t]);
         unit[t] = a.scale * 1.44269504088896340736f;
-        float v[KM][8], top = 0.0f;
-        const int rr = min(r, ka.rows - 1), i = rr / a.G, hq = h * a.G + rr - i * a.G;
-        const int64_t at = (int64_t)b * a.q_stride[0] + (int64_t)hq * a.q_stride[1] + (int64_t)i * a.q_stride[2] + kg * (D / 4);
-#pragma unroll
-        for (int k = 0; k < KM; ++k) {
-            load_q8(a, at + 8 * k, v[k]);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(v[k][j]));
-        }
+        int down = 0;
         if constexpr (QMODE != CSR_F16) {
-            top = fmaxf(top, __shfl_xor(top, 16, 64));
-            top = fmaxf(top, __shfl_xor(top, 32, 64));
-            const int e = top > 0.0f && top < INFINITY ? ilogbf(top) - 14 : 0;   // the largest to 2^14 .. 2^15
-            unit[t] = ldexpf(unit[t], e);
+            float most = 0.0f;
 #pragma unroll
             for (int k = 0; k < KM; ++k)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[k][j] = ldexpf(v[k][j], -e);
+                for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(channel_of<QMODE>(stored[t][k], j)));
+            most = fmaxf(most, __shfl_xor(most, 16, 64));
+            most = fmaxf(most, __shfl_xor(most, 32, 64));
+            down = most > 0.0f && most < INFINITY ? 14 - ilogbf(most) : 0;   // the largest to 2^14 .. 2^15
+            unit[t] = ldexpf(unit[t], -down);
         }
 #pragma unroll
         for (int k = 0; k < KM; ++k) {
             half8v hi, lo;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {   // places 2 j, 2 j + 1 of a word: nibbles j, j + 4
-                const float f = v[k][(j & 1) * 4 + (j >> 1)];
+                float f = channel_of<QMODE>(stored[t][k], (j & 1) * 4 + (j >> 1));
+                if constexpr (QMODE != CSR_F16) f = ldexpf(f, down);
                 hi[j] = (_Float16)f;
                 lo[j] = (_Float16)(f - (float)hi[j]);
             }
@@ -207,23 +245,12 @@ __global__ __launch_bounds__(64 * W, NR == 1 ? 3 : 2) void q4_stream_kernel(Attn
         }
     }
 
-    const size_t block = (size_t)bh * a.T;
-    const uint32_t T = (uint32_t)a.T, token = 8 * (m >> 2) + (m & 3);
-    const Lane at{token * (D / 2) + kg * (D / 8), ((uint32_t)(kg * (D / 4) / a.group_k) * T + token) * 4,
-                  (uint32_t)(8 * kg * (D / 2) + m * (D / 32)), ((uint32_t)(m * UC / a.group_v) * T + 8 * kg) * 4};
-
     float4v o[NR][UC] = {};
     float top[NR], sum[NR];
 #pragma unroll
     for (int t = 0; t < NR; ++t) { top[t] = kNone; sum[t] = 0.0f; }
 
-    Raw<D> next;
-    int tb = begin + wave * kStep;
-    if (tb < end) request<D>(next, a, block, at, tb, m, kg);
-    for (; tb < end; tb += kStep * W) {
-        Raw<D> r = next;
-        if (tb + kStep * W < end) request<D>(next, a, block, at, tb + kStep * W, m, kg);
-
+    const auto turn = [&](Raw<D> &r) __attribute__((always_inline)) {
         half8v k8[2][KM];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -297,14 +324,18 @@ __global__ __launch_bounds__(64 * W, NR == 1 ? 3 : 2) void q4_stream_kernel(Attn
 #pragma unroll
                 for (int c = 0; c < UC; ++c) o[t][c] *= fade;
             }
-            const float base = kShift - top[t];
+            const float lift = kShift - top[t];
+            half2v high[4], low[4];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float p = __builtin_amdgcn_exp2f(fmaf(score[t][j], unit[t], base));
-                sum[t] += p;
-                ph[t][j] = (_Float16)p;
-                pl[t][j] = (_Float16)fmaf((float)ph[t][j], -1.0f, p);
+            for (int j = 0; j < 4; ++j) {
+                const float p0 = __builtin_amdgcn_exp2f(fmaf(score[t][2 * j], unit[t], lift));
+                const float p1 = __builtin_amdgcn_exp2f(fmaf(score[t][2 * j + 1], unit[t], lift));
+                sum[t] += p0 + p1;
+                high[j] = half2v{(_Float16)p0, (_Float16)p1};
+                low[j] = half2v{(_Float16)less_low(p0, as_u32(high[j])), (_Float16)less_high(p1, as_u32(high[j]))};
             }
+            ph[t] = join(high[0], high[1], high[2], high[3]);
+            pl[t] = join(low[0], low[1], low[2], low[3]);
         }
         half2v vs[4], vm[4];
         uint32_t lo[4], hi[4];
@@ -336,6 +367,15 @@ __global__ __launch_bounds__(64 * W, NR == 1 ? 3 : 2) void q4_stream_kernel(Attn
             channel(std::integral_constant<int, 6>{});
             channel(std::integral_constant<int, 7>{});
         }
+    };
+    while (tb < end) {   // two sets of registers in turn: one is used while the other is filled
+        if (tb + kStep * W < end) request<D>(odd, cache, at, tb + kStep * W, m, kg);
+        turn(even);
+        tb += kStep * W;
+        if (tb >= end) break;
+        if (tb + kStep * W < end) request<D>(even, cache, at, tb + kStep * W, m, kg);
+        turn(odd);
+        tb += kStep * W;
     }
 
     // the waves' parts of a row tile, one tile after the other
@@ -356,72 +396,88 @@ __global__ __launch_bounds__(64 * W, NR == 1 ? 3 : 2) void q4_stream_kernel(Attn
             for (int c = 0; c < UC; c += 4)
                 *reinterpret_cast<float4v *>(&part[wave][m][(4 * kg + j) * UC + c]) = float4v{o[t][c][j], o[t][c + 1][j], o[t][c + 2][j], o[t][c + 3][j]};
         __syncthreads();
-        for (int e = threadIdx.x; e < 16 * D; e += 64 * W) {
-            const int n = e / D, ch = e - n * D, r = row0 + 16 * t + n;
+        for (int e = threadIdx.x; e < 16 * D / 4; e += 64 * W) {
+            const int n = e / (D / 4), ch = 4 * (e % (D / 4)), r = row0 + 16 * t + n;
             if (r >= row_end) break;   // (rows ascend with e)
-            float best = kNone, all = 0.0f, value = 0.0f;
+            float best = kNone, all = 0.0f;
+            float4v value = {};
 #pragma unroll
             for (int w = 0; w < W; ++w) best = fmaxf(best, parts_top[w][n]);
 #pragma unroll
             for (int w = 0; w < W; ++w) {
                 const float fade = __builtin_amdgcn_exp2f(parts_top[w][n] - best);
                 all = fmaf(parts_sum[w][n], fade, all);
-                value = fmaf(part[w][n][ch], fade, value);
+                value += *reinterpret_cast<const float4v *>(&part[w][n][ch]) * fade;
             }
             if (ka.splits == 1) {
-                const int i = r / a.G, hq = h * a.G + r - i * a.G;
-                store_out(a, (int64_t)b * a.out_stride[0] + (int64_t)hq * a.out_stride[1] + (int64_t)i * a.out_stride[2] + ch,
-                          all == 0.0f ? 0.0f : value / all);
+                const int i = quotient(r, ka.by_group), hq = h * a.G + r - i * a.G;
+                store_out4(a, (int64_t)b * a.out_stride[0] + (int64_t)hq * a.out_stride[1] + (int64_t)i * a.out_stride[2] + ch,
+                           all == 0.0f ? float4v{} : value / all);
             } else {
-                const size_t at = ((size_t)bh * ka.splits + split) * ka.rows + r;
-                ka.acc[at * D + ch] = value;
+                const size_t to = ((size_t)bh * ka.splits + split) * ka.rows + r;
+                *reinterpret_cast<float4v *>(ka.acc + to * D + ch) = value;
                 if (ch == 0) {
-                    ka.ml[2 * at] = best;
-                    ka.ml[2 * at + 1] = all;
+                    ka.ml[2 * to] = best;
+                    ka.ml[2 * to + 1] = all;
                 }
             }
         }
     }
 }
 
-// Joins the parts of the token axis: a wave per query row
+// Joins the parts of the token axis: a wave per query row, all its parts' requests ahead of their use
 template <int D>
 __global__ __launch_bounds__(256) void q4_join_kernel(AttnKernelArgs ka)
 {
-    constexpr int CH = D / 64;
+    constexpr int LANES = D / 4, SIDE = 64 / LANES, DEEP = 8;   // of a part's row; parts side by side; requests ahead
     const Q4AttnArgs &a = ka.a;
-    const int lane = threadIdx.x & 63;
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (row >= (int64_t)a.B * a.Hkv * ka.rows) return;
-    const int bh = (int)(row / ka.rows), r = (int)(row - (int64_t)bh * ka.rows), b = bh / a.Hkv, h = bh - b * a.Hkv;
+    const int lane = threadIdx.x & 63, b = blockIdx.z, h = blockIdx.y, bh = b * a.Hkv + h;
+    const int r = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (r >= ka.rows) return;
+    const int side = lane / LANES, ch = 4 * (lane % LANES);
     const size_t first = (size_t)bh * ka.splits * ka.rows + r;
-    float best = kNone, all = 0.0f, value[CH] = {};
+    float best = kNone, all = 0.0f;
+    float4v value = {};
     for (int k = lane; k < ka.splits; k += 64) best = fmaxf(best, ka.ml[2 * (first + (size_t)k * ka.rows)]);
 #pragma unroll
     for (int w = 32; w >= 1; w >>= 1) best = fmaxf(best, __shfl_xor(best, w, 64));
-    for (int k = 0; k < ka.splits; ++k) {
-        const size_t at = first + (size_t)k * ka.rows;
-        const float fade = __builtin_amdgcn_exp2f(ka.ml[2 * at] - best);
-        all = fmaf(ka.ml[2 * at + 1], fade, all);
+    for (int k0 = side; k0 < ka.splits; k0 += SIDE * DEEP) {
+        float4v part[DEEP];
+        float top[DEEP], sum[DEEP];
 #pragma unroll
-        for (int c = 0; c < CH; ++c) value[c] = fmaf(ka.acc[at * D + lane * CH + c], fade, value[c]);
+        for (int k = 0; k < DEEP; ++k) {
+            const size_t from = first + (size_t)min(k0 + SIDE * k, ka.splits - 1) * ka.rows;
+            part[k] = *reinterpret_cast<const float4v *>(ka.acc + from * D + ch);
+            top[k] = ka.ml[2 * from];
+            sum[k] = ka.ml[2 * from + 1];
+        }
+#pragma unroll
+        for (int k = 0; k < DEEP; ++k) {
+            if (k0 + SIDE * k >= ka.splits) break;
+            const float fade = __builtin_amdgcn_exp2f(top[k] - best);
+            all = fmaf(sum[k], fade, all);
+            value += part[k] * fade;
+        }
     }
-    const int i = r / a.G, hq = h * a.G + r - i * a.G;
-    const int64_t at = (int64_t)b * a.out_stride[0] + (int64_t)hq * a.out_stride[1] + (int64_t)i * a.out_stride[2] + lane * CH;
 #pragma unroll
-    for (int c = 0; c < CH; ++c) store_out(a, at + c, all == 0.0f ? 0.0f : value[c] / all);
+    for (int w = LANES; w < 64; w <<= 1) {
+        all += __shfl_xor(all, w, 64);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) value[c] += __shfl_xor(value[c], w, 64);
+    }
+    if (side != 0) return;
+    const int i = quotient(r, ka.by_group), hq = h * a.G + r - i * a.G;
+    store_out4(a, (int64_t)b * a.out_stride[0] + (int64_t)hq * a.out_stride[1] + (int64_t)i * a.out_stride[2] + ch, all == 0.0f ? float4v{} : value / all);
 }
 
 constexpr int kWaves = 4;
 
 template <int D, int QMODE, int NR> hipError_t run(const AttnKernelArgs &ka)
 {
-    const int64_t groups = (int64_t)ka.a.B * ka.a.Hkv * ka.splits * ka.row_blocks;
-    hipLaunchKernelGGL((q4_stream_kernel<D, QMODE, NR, kWaves>), dim3((unsigned)groups), dim3(64 * kWaves), 0, ka.a.stream, ka);
+    hipLaunchKernelGGL((q4_stream_kernel<D, QMODE, NR, kWaves>), dim3(ka.splits * ka.row_blocks, ka.a.Hkv, ka.a.B), dim3(64 * kWaves), 0, ka.a.stream, ka);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || ka.splits == 1) return e;
-    const int64_t rows = (int64_t)ka.a.B * ka.a.Hkv * ka.rows;
-    hipLaunchKernelGGL((q4_join_kernel<D>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, ka.a.stream, ka);
+    hipLaunchKernelGGL((q4_join_kernel<D>), dim3((ka.rows + 3) / 4, ka.a.Hkv, ka.a.B), dim3(256), 0, ka.a.stream, ka);
     return hipGetLastError();
 }
 template <int D, int QMODE> hipError_t run(const AttnKernelArgs &ka, int row_tiles)
@@ -439,24 +495,43 @@ template <int D> hipError_t run(const AttnKernelArgs &ka, int row_tiles)
 
 }  // namespace
 
+// Parts of the token axis.  What a call takes is close to (us, fitted to 11 shapes of 8 to 512 (sequence, KV head) pairs and 128
+// to 8192 tokens, each at 5 to 10 numbers of parts; off by 12 % at most)
+//   4.0 + turns * (0.2 + 0.72 * c) * size                        turns: of 128 tokens per workgroup, c: workgroups per CU
+//   + where there are parts, 2.8 + 0.1 * parts and the parts' bytes at 4 TB/s, out and in.
+// Measured at 8 pairs of 517 tokens: 7.9 us in one part, 8.3 in three; of 8192: 55.6 in one, 14.0 in eight, 11.9 in 16, 12.1 in
+// 24; 512 pairs of 2048: 28.7 in one, 32.3 in two, 35.5 in eight.
 void plan_q4_attn(const Q4AttnArgs &a, Q4AttnPlan *p)
 {
-    const int64_t rows = (int64_t)a.G * a.Tq, blocks = (int64_t)a.B * a.Hkv;
+    const int64_t rows = (int64_t)a.G * a.Tq, blocks = (int64_t)a.B * a.Hkv, step = kStep * kWaves;
     p->row_tiles = rows <= 16 ? 1 : 2;
     p->row_blocks = (int32_t)((rows + 16 * p->row_tiles - 1) / (16 * p->row_tiles));
-    const int64_t groups = blocks * p->row_blocks, fill = 1024, by_tokens = (a.T + 255) / 256;
-    int64_t splits = groups ? (fill + groups - 1) / groups : 1;
-    if (splits > by_tokens) splits = by_tokens;
-    if (splits < 1) splits = 1;
-    p->splits = (int32_t)splits;
-    const size_t parts = (size_t)blocks * (size_t)rows * (size_t)splits;
-    p->off_ml = splits > 1 ? (parts * a.d * 4 + 255) / 256 * 256 : 0;
-    p->total_bytes = splits > 1 ? p->off_ml + (parts * 8 + 255) / 256 * 256 : 0;
+    const float size = (a.d == 64 ? 0.6f : 1.0f) * (p->row_tiles == 1 ? 1.0f : 1.4f);
+    float least = INFINITY;
+    for (const int32_t splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 192, 256}) {
+        if (splits > 1 && splits > (a.T + step - 1) / step) break;
+        const int64_t turns = (a.T + step * splits - 1) / (step * splits), per_cu = (blocks * p->row_blocks * splits + kCus - 1) / kCus;
+        const float join = splits == 1 ? 0.0f : 2.8f + 0.1f * splits + (float)(blocks * rows * splits) * a.d * 8 / 4e6f;
+        const float cost = 4.0f + turns * (0.2f + 0.72f * per_cu) * size + join;
+        if (cost < least) {
+            least = cost;
+            p->splits = splits;
+        }
+    }
+    const size_t parts = (size_t)blocks * (size_t)rows * (size_t)p->splits;
+    p->off_ml = p->splits > 1 ? (parts * a.d * 4 + 255) / 256 * 256 : 0;
+    p->total_bytes = p->splits > 1 ? p->off_ml + (parts * 8 + 255) / 256 * 256 : 0;
 }
 
 hipError_t launch_q4_attn(const Q4AttnArgs &a, const Q4AttnPlan &p)
 {
-    AttnKernelArgs ka{a, p.splits, p.row_blocks, a.G * a.Tq, static_cast<float *>(a.workspace), nullptr};
+    AttnKernelArgs ka{};
+    const auto log2_of = [](int32_t group) { return group == 32 ? 5 : group == 64 ? 6 : 7; };
+    ka.a = a;
+    ka.splits = p.splits; ka.row_blocks = p.row_blocks; ka.rows = a.G * a.Tq;
+    ka.log_group_k = log2_of(a.group_k); ka.log_group_v = log2_of(a.group_v);
+    ka.by_splits = fast_div((uint32_t)p.splits); ka.by_group = fast_div((uint32_t)a.G);
+    ka.acc = static_cast<float *>(a.workspace);
     ka.ml = reinterpret_cast<float *>(static_cast<char *>(a.workspace) + p.off_ml);
     return a.d == 128 ? run<128>(ka, p.row_tiles) : run<64>(ka, p.row_tiles);
 }

@@ -50,12 +50,29 @@ __device__ __forceinline__ bool not_finite(uint32_t sm)
     return (sm & 0x7c00u) == 0x7c00u || (sm & 0x7c000000u) == 0x7c000000u;
 }
 
-__device__ __forceinline__ float bf16_to_float(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
 __device__ __forceinline__ uint16_t float_to_bf16(float f)   // to nearest, halves to even; a NaN stays one
 {
     const uint32_t u = __float_as_uint(f);
     if ((u & 0x7fffffffu) > 0x7f800000u) return (uint16_t)((u >> 16) | 0x40u);
     return (uint16_t)((u + 0x7fffu + ((u >> 16) & 1u)) >> 16);
+}
+
+// Unsigned division by a number that the host knows: x / d = (x * mul) >> (32 + shift) for x below 2^31
+struct FastDiv {
+    uint32_t mul, shift, div;
+};
+inline FastDiv fast_div(uint32_t d)
+{
+    FastDiv f{0, 0, d};
+    if (d == 1) return f;
+    while ((1ull << f.shift) < d) ++f.shift;   // ceil(log2 d): mul < 2^32, and the error stays below 1 / d for x < 2^31
+    --f.shift;
+    f.mul = (uint32_t)(((1ull << (32 + f.shift)) + d - 1) / d);
+    return f;
+}
+__device__ __forceinline__ uint32_t quotient(uint32_t x, const FastDiv &f)
+{
+    return f.div == 1 ? x : __umulhi(x, f.mul) >> f.shift;
 }
 
 }  // namespace q4

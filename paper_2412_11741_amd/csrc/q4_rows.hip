@@ -15,24 +15,6 @@ using namespace q4;
 
 constexpr float kLargest = 65504.0f;   // of fp16
 
-// Unsigned division by a number that the host knows: x / d = (x * mul) >> (32 + shift) for x below 2^31
-struct FastDiv {
-    uint32_t mul, shift, div;
-};
-FastDiv fast_div(uint32_t d)
-{
-    FastDiv f{0, 0, d};
-    if (d == 1) return f;
-    while ((1ull << f.shift) < d) ++f.shift;   // ceil(log2 d): mul < 2^32, and the error stays below 1 / d for x < 2^31
-    --f.shift;
-    f.mul = (uint32_t)(((1ull << (32 + f.shift)) + d - 1) / d);
-    return f;
-}
-__device__ __forceinline__ uint32_t quotient(uint32_t x, const FastDiv &f)
-{
-    return f.div == 1 ? x : __umulhi(x, f.mul) >> f.shift;
-}
-
 struct RowsSide {
     const void *x;
     uint32_t *codes;   // words of eight channels
