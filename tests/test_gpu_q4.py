@@ -61,7 +61,7 @@ def _blank(B, Hkv, T, d, group):
 # ---- write and read -----------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("dtype", [F16, BF16, F32])
 @pytest.mark.parametrize("d,group", [(128, 32), (128, 64), (128, 128), (64, 32), (64, 64)])
-@pytest.mark.parametrize("B,Hkv,n,T", [(1, 1, 1, 1), (2, 3, 37, 50), (3, 5, 1, 9), (1, 2, 517, 600)])
+@pytest.mark.parametrize("B,Hkv,n,T", [(1, 1, 1, 1), (2, 3, 37, 50), (3, 5, 1, 9), (1, 2, 517, 600), (2, 8, 1500, 1501)])
 def test_written_rows_are_the_definitions(dtype, d, group, B, Hkv, n, T):
     gain = 10.0 ** torch.randint(-4, 4, (B, Hkv, n, 1), device="cuda", generator=_gen(n)).float()
     K, V = _randn(1, B, Hkv, n, d, dtype=dtype, gain=gain), _token_major(_randn(2, B, Hkv, n, d, dtype=dtype))
