@@ -12,9 +12,10 @@
 //   - lane (m, kg) takes the channels 32 kg .. of token m's key (d / 4 of them: one or two words, one group of the scale);
 //   - a lane's four scores of either half of the 32 tokens are tokens 8 kg .. 8 kg + 7 and go into the next product as they are;
 //   - lane (m, kg) takes channels (d / 16) m .. of the values of tokens 8 kg .. 8 kg + 7: two tokens' words are cut into halves and
-//     joined, and every nibble pair is then one channel of two tokens.
+//     joined, and every pair of codes is then one channel of two tokens.
 // Probabilities are relative to 2^13 below the running maximum (and the maximum is only moved when it is passed by 2^2), so that
 // as two fp16 - the value and what it lacks - they keep 22 bits down to 2^-27 of the largest, and the rest to 2^-37.
+#include <cfloat>
 #include <cmath>
 #include <type_traits>
 
@@ -130,11 +131,9 @@ struct Lane {
 typedef uint4v uint4a __attribute__((aligned(4)));
 
 // WHOLE: all 32 tokens are rows of the cache.  Else rows behind the last one are requested as the last one.
-template <int D, bool WHOLE>
-__device__ __forceinline__ void request(Raw<D> &r, const Base &base, const Lane &at, int tb, int m, int kg)
+template <int D, bool WHOLE> __device__ __forceinline__ void request_keys(Raw<D> &r, const Base &base, const Lane &at, int tb, int m)
 {
-    const uint8_t *kc = base.kc + (uint32_t)tb * (D / 2), *vc = base.vc + (uint32_t)tb * (D / 2);
-    const uint8_t *kp = base.kp + (uint32_t)tb * 4, *vp = base.vp + (uint32_t)tb * 4;
+    const uint8_t *kc = base.kc + (uint32_t)tb * (D / 2), *kp = base.kp + (uint32_t)tb * 4;
     const int last = base.T - 1 - tb;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
@@ -151,6 +150,11 @@ __device__ __forceinline__ void request(Raw<D> &r, const Base &base, const Lane 
         }
         r.kp[u] = *reinterpret_cast<const uint32_t *>(kp + (at.kp + 16 * u - back * 4));
     }
+}
+template <int D, bool WHOLE> __device__ __forceinline__ void request_values(Raw<D> &r, const Base &base, const Lane &at, int tb, int kg)
+{
+    const uint8_t *vc = base.vc + (uint32_t)tb * (D / 2), *vp = base.vp + (uint32_t)tb * 4;
+    const int last = base.T - 1 - tb;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const int back = WHOLE ? 0 : max(0, 8 * kg + j - last);
@@ -165,11 +169,20 @@ __device__ __forceinline__ void request(Raw<D> &r, const Base &base, const Lane 
         for (int j = 0; j < 4; ++j) { r.vp[j] = w0[j]; r.vp[4 + j] = w1[j]; }
     }
 }
-template <int D>
-__device__ __forceinline__ void request(Raw<D> &r, const Base &base, const Lane &at, int tb, int m, int kg)
+template <int D> __device__ __forceinline__ void request_keys(Raw<D> &r, const Base &base, const Lane &at, int tb, int m)
 {
-    if (tb + kStep <= base.T) request<D, true>(r, base, at, tb, m, kg);
-    else request<D, false>(r, base, at, tb, m, kg);
+    if (tb + kStep <= base.T) request_keys<D, true>(r, base, at, tb, m);
+    else request_keys<D, false>(r, base, at, tb, m);
+}
+template <int D> __device__ __forceinline__ void request_values(Raw<D> &r, const Base &base, const Lane &at, int tb, int kg)
+{
+    if (tb + kStep <= base.T) request_values<D, true>(r, base, at, tb, kg);
+    else request_values<D, false>(r, base, at, tb, kg);
+}
+template <int D> __device__ __forceinline__ void request(Raw<D> &r, const Base &base, const Lane &at, int tb, int m, int kg)
+{
+    request_keys<D>(r, base, at, tb, m);
+    request_values<D>(r, base, at, tb, kg);
 }
 
 // QMODE: csr_dtype of q.  NR: tiles of 16 query rows.  W: waves.
@@ -179,6 +192,9 @@ __global__ __launch_bounds__(64 * W, NR == 1 && QMODE != CSR_F32 ? 3 : 2) void q
     constexpr int KM = D / 32;   // matrix instructions along a key's channels
     constexpr int UC = D / 16;   // channels of a lane's values
     constexpr bool kTwo = QMODE == CSR_F32;
+    constexpr bool kMany = NR == 4;        // queries wait in LDS, probabilities are one fp16
+    constexpr bool kOneSet = kMany || (kTwo && NR == 2);   // of registers for requests: two do not fit
+    static_assert(!kMany || (W == 4 && !kTwo), "a wave converts one tile of queries");
     const Q4AttnArgs &a = ka.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, kg = lane >> 4;
     const int b = blockIdx.z, h = blockIdx.y, bh = b * a.Hkv + h;
@@ -186,12 +202,11 @@ __global__ __launch_bounds__(64 * W, NR == 1 && QMODE != CSR_F32 ? 3 : 2) void q
     const int row0 = rb * 16 * NR, row_end = min(row0 + 16 * NR, ka.rows);
     const int len = a.seq_lens ? a.seq_lens[b] : (int)a.T, qn = a.q_lens ? a.q_lens[b] : a.Tq;
 
-    Stored8<QMODE> stored[NR][KM];
-    int query[NR];
+    constexpr int NC = kMany ? 1 : NR;   // tiles of queries that a wave converts
+    Stored8<QMODE> stored[NC][KM];
 #pragma unroll
-    for (int t = 0; t < NR; ++t) {
-        const int r = min(row0 + 16 * t + m, ka.rows - 1), i = quotient(r, ka.by_group);
-        query[t] = row0 + 16 * t + m < ka.rows ? i : a.Tq;
+    for (int t = 0; t < NC; ++t) {
+        const int r = min(row0 + 16 * (kMany ? wave : t) + m, ka.rows - 1), i = quotient(r, ka.by_group);
         const int64_t from = (int64_t)b * a.q_stride[0] + (int64_t)(h * a.G + r - i * a.G) * a.q_stride[1] + (int64_t)i * a.q_stride[2] + kg * (D / 4);
 #pragma unroll
         for (int k = 0; k < KM; ++k) load_q8<QMODE>(stored[t][k], a.q, from + 8 * k);
@@ -211,12 +226,13 @@ __global__ __launch_bounds__(64 * W, NR == 1 && QMODE != CSR_F32 ? 3 : 2) void q
     if (tb < end) request<D>(even, cache, at, tb, m, kg);
 
     // the queries: fp16, and what that lacks; in units that leave no loss to bf16
-    half8v qh[NR][KM], ql[kTwo ? NR : 1][KM];
+    __shared__ half8v waiting[kMany ? NR * KM * 64 : 1];
+    __shared__ float waiting_unit[kMany ? NR * 16 : 1];
+    half8v qh[NC][KM], ql[kTwo ? NC : 1][KM];
     float unit[NR];
     int limit[NR];
 #pragma unroll
-    for (int t = 0; t < NR; ++t) {
-        limit[t] = limit_of(ka, s, query[t]);
+    for (int t = 0; t < NC; ++t) {
         unit[t] = a.scale * 1.44269504088896340736f;
         int down = 0;
         if constexpr (QMODE != CSR_F16) {
@@ -230,19 +246,32 @@ __global__ __launch_bounds__(64 * W, NR == 1 && QMODE != CSR_F32 ? 3 : 2) void q
             down = most > 0.0f && most < INFINITY ? 14 - ilogbf(most) : 0;   // the largest to 2^14 .. 2^15
             unit[t] = ldexpf(unit[t], -down);
         }
+        unit[t] = fminf(fmaxf(unit[t], FLT_MIN), FLT_MAX);   // (an unseen token's score, minus infinity, times 0 would be no number)
 #pragma unroll
         for (int k = 0; k < KM; ++k) {
             half8v hi, lo;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {   // places 2 j, 2 j + 1 of a word: nibbles j, j + 4
-                float f = channel_of<QMODE>(stored[t][k], (j & 1) * 4 + (j >> 1));
+            for (int j = 0; j < 8; ++j) {   // in the order that a word's channels come in: 0, 2, 4, 6, 1, 3, 5, 7
+                float f = channel_of<QMODE>(stored[t][k], 2 * (j & 3) + (j >> 2));
                 if constexpr (QMODE != CSR_F16) f = ldexpf(f, down);
                 hi[j] = (_Float16)f;
                 lo[j] = (_Float16)(f - (float)hi[j]);
             }
             qh[t][k] = hi;
             if constexpr (kTwo) ql[t][k] = lo;
+            if constexpr (kMany) waiting[(wave * KM + k) * 64 + lane] = hi;
         }
+    }
+    if constexpr (kMany) {
+        if (kg == 0) waiting_unit[16 * wave + m] = unit[0];
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < NR; ++t) unit[t] = waiting_unit[16 * t + m];
+    }
+#pragma unroll
+    for (int t = 0; t < NR; ++t) {
+        const int r = row0 + 16 * t + m;
+        limit[t] = r < ka.rows ? limit_of(ka, s, quotient(r, ka.by_group)) : -1;
     }
 
     float4v o[NR][UC] = {};
@@ -257,23 +286,29 @@ __global__ __launch_bounds__(64 * W, NR == 1 && QMODE != CSR_F32 ? 3 : 2) void q
             const half2v ks = as_half2(low_halves(r.kp[u], r.kp[u])), km = as_half2(high_halves(r.kp[u], r.kp[u]));
 #pragma unroll
             for (int k = 0; k < KM; ++k)
-                k8[u][k] = join(fma2(nibble_pair<0>(r.kc[u][k]), ks, km), fma2(nibble_pair<1>(r.kc[u][k]), ks, km),
-                                fma2(nibble_pair<2>(r.kc[u][k]), ks, km), fma2(nibble_pair<3>(r.kc[u][k]), ks, km));
+                k8[u][k] = join(fma2(whole2<false>(evens(r.kc[u][k])), ks, km), fma2(whole2<true>(evens(r.kc[u][k])), ks, km),
+                                fma2(whole2<false>(odds(r.kc[u][k])), ks, km), fma2(whole2<true>(odds(r.kc[u][k])), ks, km));
         }
         float score[NR][8];
+        int from = lane;   // (the queries are read every turn: held back, they would push other values out of the registers)
+        asm volatile("" : "+v"(from));
 #pragma unroll
-        for (int t = 0; t < NR; ++t)
+        for (int t = 0; t < NR; ++t) {
+            float4v c[2] = {};
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                float4v c = {};
+            for (int k = 0; k < KM; ++k) {
+                const half8v q = kMany ? waiting[(t * KM + k) * 64 + from] : qh[kMany ? 0 : t][k];
 #pragma unroll
-                for (int k = 0; k < KM; ++k) {
-                    c = mfma(k8[u][k], qh[t][k], c);
-                    if constexpr (kTwo) c = mfma(k8[u][k], ql[t][k], c);
+                for (int u = 0; u < 2; ++u) {
+                    c[u] = mfma(k8[u][k], q, c[u]);
+                    if constexpr (kTwo) c[u] = mfma(k8[u][k], ql[t][k], c[u]);
                 }
-#pragma unroll
-                for (int j = 0; j < 4; ++j) score[t][4 * u + j] = c[j];
             }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) score[t][j] = c[j / 4][j % 4];
+        }
+        if constexpr (kOneSet)
+            if (tb + kStep * W < end) request_keys<D>(r, cache, at, tb + kStep * W, m);
         // tokens that some row does not see: out of its scores, and values that are no finite numbers out of the product - the
         // rows that do see them get NaN
         if (tb + kStep > s.all) {
@@ -307,7 +342,7 @@ __global__ __launch_bounds__(64 * W, NR == 1 && QMODE != CSR_F32 ? 3 : 2) void q
                 }
             }
         }
-        half8v ph[NR], pl[NR];
+        half8v ph[NR], pl[kMany ? 1 : NR];
 #pragma unroll
         for (int t = 0; t < NR; ++t) {
             float best = score[t][0];
@@ -325,36 +360,41 @@ __global__ __launch_bounds__(64 * W, NR == 1 && QMODE != CSR_F32 ? 3 : 2) void q
                 for (int c = 0; c < UC; ++c) o[t][c] *= fade;
             }
             const float lift = kShift - top[t];
-            half2v high[4], low[4];
+            half2v p2[4], rest[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const float p0 = __builtin_amdgcn_exp2f(fmaf(score[t][2 * j], unit[t], lift));
                 const float p1 = __builtin_amdgcn_exp2f(fmaf(score[t][2 * j + 1], unit[t], lift));
                 sum[t] += p0 + p1;
-                high[j] = half2v{(_Float16)p0, (_Float16)p1};
-                low[j] = half2v{(_Float16)less_low(p0, as_u32(high[j])), (_Float16)less_high(p1, as_u32(high[j]))};
+                p2[j] = half2v{(_Float16)p0, (_Float16)p1};
+                if constexpr (!kMany) rest[j] = half2v{(_Float16)less_low(p0, as_u32(p2[j])), (_Float16)less_high(p1, as_u32(p2[j]))};
             }
-            ph[t] = join(high[0], high[1], high[2], high[3]);
-            pl[t] = join(low[0], low[1], low[2], low[3]);
+            ph[t] = join(p2[0], p2[1], p2[2], p2[3]);
+            if constexpr (!kMany) pl[t] = join(rest[0], rest[1], rest[2], rest[3]);
         }
         half2v vs[4], vm[4];
-        uint32_t lo[4], hi[4];
+        uint32_t low[4], high[4];   // channels 0 .. 3 and 4 .. 7 of two tokens
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             vs[j] = as_half2(low_halves(r.vp[2 * j], r.vp[2 * j + 1]));
             vm[j] = as_half2(high_halves(r.vp[2 * j], r.vp[2 * j + 1]));
-            lo[j] = low_halves(r.vc[2 * j], r.vc[2 * j + 1]);
-            hi[j] = high_halves(r.vc[2 * j], r.vc[2 * j + 1]);
+            low[j] = low_bytes(r.vc[2 * j], r.vc[2 * j + 1]);
+            high[j] = high_bytes(r.vc[2 * j], r.vc[2 * j + 1]);
         }
         const auto channel = [&](auto c) {
-            constexpr int C = decltype(c)::value, N = C & 3;
-            const uint32_t(&w)[4] = C < 4 ? lo : hi;
-            const half8v v8 = join(fma2(nibble_pair<N>(w[0]), vs[0], vm[0]), fma2(nibble_pair<N>(w[1]), vs[1], vm[1]),
-                                   fma2(nibble_pair<N>(w[2]), vs[2], vm[2]), fma2(nibble_pair<N>(w[3]), vs[3], vm[3]));
+            constexpr int C = decltype(c)::value;
+            constexpr bool UPPER = (C & 2) != 0;
+            half2v v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t w = C < 4 ? low[j] : high[j];
+                v[j] = fma2(whole2<UPPER>(C & 1 ? odds(w) : evens(w)), vs[j], vm[j]);
+            }
+            const half8v v8 = join(v[0], v[1], v[2], v[3]);
 #pragma unroll
             for (int t = 0; t < NR; ++t) {
                 o[t][C] = mfma(v8, ph[t], o[t][C]);
-                o[t][C] = mfma(v8, pl[t], o[t][C]);
+                if constexpr (!kMany) o[t][C] = mfma(v8, pl[t], o[t][C]);
             }
         };
         channel(std::integral_constant<int, 0>{});
@@ -368,14 +408,21 @@ __global__ __launch_bounds__(64 * W, NR == 1 && QMODE != CSR_F32 ? 3 : 2) void q
             channel(std::integral_constant<int, 7>{});
         }
     };
-    while (tb < end) {   // two sets of registers in turn: one is used while the other is filled
-        if (tb + kStep * W < end) request<D>(odd, cache, at, tb + kStep * W, m, kg);
-        turn(even);
-        tb += kStep * W;
-        if (tb >= end) break;
-        if (tb + kStep * W < end) request<D>(even, cache, at, tb + kStep * W, m, kg);
-        turn(odd);
-        tb += kStep * W;
+    if constexpr (kOneSet) {   // one set of registers, filled again as soon as it has been read
+        for (; tb < end; tb += kStep * W) {
+            turn(even);
+            if (tb + kStep * W < end) request_values<D>(even, cache, at, tb + kStep * W, kg);
+        }
+    } else {
+        while (tb < end) {   // two sets in turn: one is used while the other is filled
+            if (tb + kStep * W < end) request<D>(odd, cache, at, tb + kStep * W, m, kg);
+            turn(even);
+            tb += kStep * W;
+            if (tb >= end) break;
+            if (tb + kStep * W < end) request<D>(even, cache, at, tb + kStep * W, m, kg);
+            turn(odd);
+            tb += kStep * W;
+        }
     }
 
     // the waves' parts of a row tile, one tile after the other
@@ -482,6 +529,8 @@ template <int D, int QMODE, int NR> hipError_t run(const AttnKernelArgs &ka)
 }
 template <int D, int QMODE> hipError_t run(const AttnKernelArgs &ka, int row_tiles)
 {
+    if constexpr (QMODE != CSR_F32)
+        if (row_tiles == 4) return run<D, QMODE, 4>(ka);
     return row_tiles == 1 ? run<D, QMODE, 1>(ka) : run<D, QMODE, 2>(ka);
 }
 template <int D> hipError_t run(const AttnKernelArgs &ka, int row_tiles)
@@ -504,9 +553,9 @@ template <int D> hipError_t run(const AttnKernelArgs &ka, int row_tiles)
 void plan_q4_attn(const Q4AttnArgs &a, Q4AttnPlan *p)
 {
     const int64_t rows = (int64_t)a.G * a.Tq, blocks = (int64_t)a.B * a.Hkv, step = kStep * kWaves;
-    p->row_tiles = rows <= 16 ? 1 : 2;
+    p->row_tiles = rows <= 16 ? 1 : rows <= 32 || a.q_dtype == CSR_F32 ? 2 : 4;
     p->row_blocks = (int32_t)((rows + 16 * p->row_tiles - 1) / (16 * p->row_tiles));
-    const float size = (a.d == 64 ? 0.6f : 1.0f) * (p->row_tiles == 1 ? 1.0f : 1.4f);
+    const float size = (a.d == 64 ? 0.6f : 1.0f) * (p->row_tiles == 1 ? 1.0f : p->row_tiles == 2 ? 1.4f : 1.8f);
     float least = INFINITY;
     for (const int32_t splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 192, 256}) {
         if (splits > 1 && splits > (a.T + step - 1) / step) break;

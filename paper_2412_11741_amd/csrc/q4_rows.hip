@@ -113,12 +113,12 @@ template <int DT> __device__ __forceinline__ void widen8(const Stored8<DT> &r, f
     }
 }
 
-// Channels 0..7 from pairs (k, k + 4)
+// Channels 0..7 from pairs (0, 2), (4, 6), (1, 3), (5, 7)
 template <int DT, int MODE> __device__ __forceinline__ void store8(uint8_t *p, const half2v (&pair)[4])
 {
     if constexpr (DT == CSR_F32) {
-        const float4v v[2] = {float4v{(float)pair[0][0], (float)pair[1][0], (float)pair[2][0], (float)pair[3][0]},
-                              float4v{(float)pair[0][1], (float)pair[1][1], (float)pair[2][1], (float)pair[3][1]}};
+        const float4v v[2] = {float4v{(float)pair[0][0], (float)pair[2][0], (float)pair[0][1], (float)pair[2][1]},
+                              float4v{(float)pair[1][0], (float)pair[3][0], (float)pair[1][1], (float)pair[3][1]}};
         if constexpr (MODE == PAST) {
             // past the L2s a store has to fill its 64 bytes: the four lanes of a quad, 128 bytes, put the lower half and then the
             // upper one together (with halves of theirs each, reading back 4 x 8 x 32768 vectors took 204 us instead of 141)
@@ -143,25 +143,25 @@ template <int DT, int MODE> __device__ __forceinline__ void store8(uint8_t *p, c
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             if constexpr (DT == CSR_F16) {
-                w[k] = low_halves(as_u32(pair[2 * k]), as_u32(pair[2 * k + 1]));
-                w[2 + k] = high_halves(as_u32(pair[2 * k]), as_u32(pair[2 * k + 1]));
+                w[2 * k] = low_halves(as_u32(pair[k]), as_u32(pair[2 + k]));
+                w[2 * k + 1] = high_halves(as_u32(pair[k]), as_u32(pair[2 + k]));
             } else {
-                w[k] = (uint32_t)float_to_bf16((float)pair[2 * k][0]) | (uint32_t)float_to_bf16((float)pair[2 * k + 1][0]) << 16;
-                w[2 + k] = (uint32_t)float_to_bf16((float)pair[2 * k][1]) | (uint32_t)float_to_bf16((float)pair[2 * k + 1][1]) << 16;
+                w[2 * k] = (uint32_t)float_to_bf16((float)pair[k][0]) | (uint32_t)float_to_bf16((float)pair[2 + k][0]) << 16;
+                w[2 * k + 1] = (uint32_t)float_to_bf16((float)pair[k][1]) | (uint32_t)float_to_bf16((float)pair[2 + k][1]) << 16;
             }
         }
         put<MODE == PAST>(w, reinterpret_cast<uint4v *>(p));
     }
 }
 
-// fp16(s * code + m) of a word's eight channels, as pairs (k, k + 4)
+// fp16(s * code + m) of a word's eight channels, as pairs (0, 2), (4, 6), (1, 3), (5, 7)
 __device__ __forceinline__ void word_values(uint32_t w, uint32_t sm, half2v (&pair)[4])
 {
     const half2v s = as_half2(low_halves(sm, sm)), m = as_half2(high_halves(sm, sm));
-    pair[0] = fma2(nibble_pair<0>(w), s, m);
-    pair[1] = fma2(nibble_pair<1>(w), s, m);
-    pair[2] = fma2(nibble_pair<2>(w), s, m);
-    pair[3] = fma2(nibble_pair<3>(w), s, m);
+    pair[0] = fma2(whole2<false>(evens(w)), s, m);
+    pair[1] = fma2(whole2<true>(evens(w)), s, m);
+    pair[2] = fma2(whole2<false>(odds(w)), s, m);
+    pair[3] = fma2(whole2<true>(odds(w)), s, m);
 }
 
 // Of three, without the quieting of signalling NaNs that fminf and fmaxf put before each operand
@@ -310,9 +310,8 @@ __global__ __launch_bounds__(256) void q4_read_kernel(RowsKernelArgs a)
             w = reinterpret_cast<const uint16_t *>(p.codes)[(row << LOGW) + o];
             sm = p.params[((4 * o) >> s.log_group) * a.T + row];
         }
-        w = (w & 0xffu) | (w & 0xff00u) << 8;   // channels 0, 1 and 2, 3 of the four
         const half2v scale = as_half2(low_halves(sm, sm)), least = as_half2(high_halves(sm, sm));
-        const half2v even = fma2(nibble_pair<0>(w), scale, least), odd = fma2(nibble_pair<1>(w), scale, least);
+        const half2v even = fma2(whole2<false>(evens(w)), scale, least), odd = fma2(whole2<false>(odds(w)), scale, least);
         put<MODE == PAST>(float4v{(float)even[0], (float)odd[0], (float)even[1], (float)odd[1]}, reinterpret_cast<float4v *>(to));
     } else {
         if (held) {

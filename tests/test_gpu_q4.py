@@ -212,7 +212,7 @@ def _check(q, cache, got, seq_lens=None, q_lens=None, causal=True, scale=0.0):
     lens = [T] * B if seq_lens is None else [max(0, min(int(n), T)) for n in seq_lens]
     qn = [Tq] * B if q_lens is None else [max(0, min(int(n), Tq)) for n in q_lens]
     want, spread, size = ref.attention(_np(q4), k, v, lens, qn, scale or d ** -0.5, causal)
-    one_p = Tq * (Hq // k.shape[1]) > 64 and q.dtype != F32
+    one_p = Tq * (Hq // k.shape[1]) > 32 and q.dtype != F32
     off = np.abs(_np(g4) - want) / _bound(want, spread, size, T, d, q.dtype, got.dtype, one_p)
     assert np.isfinite(off).all() and off.max() <= 1, off.max()
     return off.max()
@@ -332,9 +332,9 @@ def test_scores_far_apart_and_large(G, Tq):
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_queries_beyond_the_range_of_fp16(dtype):
     cache = _filled(70, 1, 2, 90, 128, 64, 64)
-    for size in (1e-20, 1e-6, 3e5, 1e15):
+    for size in (1e-38, 1e-20, 1e-6, 3e5, 1e15):
         q = _randn(72, 1, 4, 128, dtype=F32, gain=size).to(dtype)
-        _check(q, cache, csr.csr_q4_attn(q, *cache, scale=0.1 / size, out_dtype=F32), scale=float(np.float32(0.1 / size)))
+        _check(q, cache, csr.csr_q4_attn(q, *cache, scale=0.1 / max(size, 1e-30), out_dtype=F32), scale=float(np.float32(0.1 / max(size, 1e-30))))
     q = torch.zeros(1, 4, 128, dtype=dtype, device="cuda")
     _check(q, cache, csr.csr_q4_attn(q, *cache, out_dtype=F32))
 
