@@ -483,21 +483,26 @@ __global__ __launch_bounds__(256) void q4_join_kernel(AttnKernelArgs ka)
     if (r >= ka.rows) return;
     const int side = lane / LANES, ch = 4 * (lane % LANES);
     const size_t first = (size_t)bh * ka.splits * ka.rows + r;
-    float best = kNone, all = 0.0f;
+    float all = 0.0f, best = kNone;
     float4v value = {};
-    for (int k = lane; k < ka.splits; k += 64) best = fmaxf(best, ka.ml[2 * (first + (size_t)k * ka.rows)]);
-#pragma unroll
-    for (int w = 32; w >= 1; w >>= 1) best = fmaxf(best, __shfl_xor(best, w, 64));
-    for (int k0 = side; k0 < ka.splits; k0 += SIDE * DEEP) {
-        float4v part[DEEP];
-        float top[DEEP], sum[DEEP];
+    float4v part[DEEP];
+    float top[DEEP], sum[DEEP];
+    const auto request = [&](int k0) {
 #pragma unroll
         for (int k = 0; k < DEEP; ++k) {
             const size_t from = first + (size_t)min(k0 + SIDE * k, ka.splits - 1) * ka.rows;
             part[k] = *reinterpret_cast<const float4v *>(ka.acc + from * D + ch);
-            top[k] = ka.ml[2 * from];
-            sum[k] = ka.ml[2 * from + 1];
+            const float2 ml = *reinterpret_cast<const float2 *>(ka.ml + 2 * from);
+            top[k] = ml.x;
+            sum[k] = ml.y;
         }
+    };
+    request(side);   // (ahead of the maxima: they come with it)
+    for (int k = lane; k < ka.splits; k += 64) best = fmaxf(best, ka.ml[2 * (first + (size_t)k * ka.rows)]);
+#pragma unroll
+    for (int w = 32; w >= 1; w >>= 1) best = fmaxf(best, __shfl_xor(best, w, 64));
+    for (int k0 = side; k0 < ka.splits; k0 += SIDE * DEEP) {
+        if (k0 != side) request(k0);
 #pragma unroll
         for (int k = 0; k < DEEP; ++k) {
             if (k0 + SIDE * k >= ka.splits) break;
@@ -544,24 +549,24 @@ template <int D> hipError_t run(const AttnKernelArgs &ka, int row_tiles)
 
 }  // namespace
 
-// Parts of the token axis.  What a call takes is close to (us, fitted to 11 shapes of 8 to 512 (sequence, KV head) pairs and 128
-// to 8192 tokens, each at 5 to 10 numbers of parts; off by 12 % at most)
-//   4.0 + turns * (0.2 + 0.72 * c) * size                        turns: of 128 tokens per workgroup, c: workgroups per CU
-//   + where there are parts, 2.8 + 0.1 * parts and the parts' bytes at 4 TB/s, out and in.
-// Measured at 8 pairs of 517 tokens: 7.9 us in one part, 8.3 in three; of 8192: 55.6 in one, 14.0 in eight, 11.9 in 16, 12.1 in
-// 24; 512 pairs of 2048: 28.7 in one, 32.3 in two, 35.5 in eight.
+// Parts of the token axis.  What a call takes is close to (us, fitted to 19 shapes of 8 to 512 (sequence, KV head) pairs and 128
+// to 8192 tokens, each at up to 10 numbers of parts)
+//   turns * (0.2 + 0.8 * c) * size    turns: of 128 tokens per workgroup, c: workgroups per CU, size: of a turn
+//   + 3.6 in one part; in more 6.7, 0.08 for every part beyond 16 and the parts' bytes at 4 TB/s, out and in.
+// Measured at 8 pairs of 517 tokens: 7.8 us in one part, 8.3 in three; of 8192: 56.4 in one, 13.5 in eight, 10.1 in 16, 10.6 in
+// 24; 512 pairs of 2048: 29.8 in one, 32.1 in two.
 void plan_q4_attn(const Q4AttnArgs &a, Q4AttnPlan *p)
 {
     const int64_t rows = (int64_t)a.G * a.Tq, blocks = (int64_t)a.B * a.Hkv, step = kStep * kWaves;
     p->row_tiles = rows <= 16 ? 1 : rows <= 32 || a.q_dtype == CSR_F32 ? 2 : 4;
     p->row_blocks = (int32_t)((rows + 16 * p->row_tiles - 1) / (16 * p->row_tiles));
-    const float size = (a.d == 64 ? 0.6f : 1.0f) * (p->row_tiles == 1 ? 1.0f : p->row_tiles == 2 ? 1.4f : 1.8f);
+    const float size = (a.d == 64 ? 0.6f : 1.0f) * (p->row_tiles == 1 ? 1.0f : p->row_tiles == 2 ? 1.36f : 2.6f);
     float least = INFINITY;
     for (const int32_t splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 192, 256}) {
         if (splits > 1 && splits > (a.T + step - 1) / step) break;
         const int64_t turns = (a.T + step * splits - 1) / (step * splits), per_cu = (blocks * p->row_blocks * splits + kCus - 1) / kCus;
-        const float join = splits == 1 ? 0.0f : 2.8f + 0.1f * splits + (float)(blocks * rows * splits) * a.d * 8 / 4e6f;
-        const float cost = 4.0f + turns * (0.2f + 0.72f * per_cu) * size + join;
+        const float join = splits == 1 ? 3.6f : 6.7f + 0.08f * (splits > 16 ? splits - 16 : 0) + (float)(blocks * rows * splits) * a.d * 8 / 4e6f;
+        const float cost = turns * (0.2f + 0.8f * per_cu) * size + join;
         if (cost < least) {
             least = cost;
             p->splits = splits;
