@@ -15,11 +15,10 @@
 //     joined, and every pair of codes is then one channel of two tokens.
 // Probabilities are relative to 2^13 below the running maximum (and the maximum is only moved when it is passed by 2^2), so that
 // as two fp16 - the value and what it lacks - they keep 22 bits down to 2^-27 of the largest, and the rest to 2^-37.
-#include <cfloat>
-#include <cmath>
 #include <type_traits>
+#include <cstdlib>
 
-#include "q4_common.h"
+#include "q4_attn_common.h"
 
 namespace csr {
 namespace {
@@ -27,9 +26,6 @@ namespace {
 using namespace q4;
 
 constexpr int kStep = 32;          // tokens of a wave's turn
-constexpr float kShift = 13.0f;    // p = 2^(score - maximum + kShift)
-constexpr float kSlack = 2.0f;     // a maximum may lag this far behind: p <= 2^15
-constexpr float kNone = -1e30f;    // a maximum before any token
 
 __device__ __forceinline__ float4v mfma(half8v a, half8v b, float4v c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
@@ -50,67 +46,6 @@ __device__ __forceinline__ float less_high(float p, uint32_t h)
     float r;
     asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(r) : "v"(h), "v"(p));
     return r;
-}
-
-struct AttnKernelArgs {
-    Q4AttnArgs a;
-    int32_t splits, row_blocks, rows;
-    int32_t log_group_k, log_group_v;
-    FastDiv by_splits, by_group;
-    float *acc, *ml;
-};
-
-// Tokens that the queries of a block see: [0, end) by some, [0, all) by all
-struct Sight {
-    int len, qn, end, all;
-};
-__device__ __forceinline__ Sight sight_of(const AttnKernelArgs &ka, int len, int qn, int row0, int row_end)
-{
-    Sight s;
-    s.len = max(0, min(len, (int)ka.a.T));
-    s.qn = max(0, min(qn, ka.a.Tq));
-    const int first = quotient(row0, ka.by_group), last = quotient(row_end - 1, ka.by_group);
-    if (first >= s.qn) { s.end = s.all = 0; return s; }
-    s.end = ka.a.causal ? max(0, s.len - s.qn + min(last, s.qn - 1) + 1) : s.len;
-    s.all = last >= s.qn ? 0 : ka.a.causal ? max(0, s.len - s.qn + first + 1) : s.len;
-    return s;
-}
-// The last token that query token i sees, -1 for none
-__device__ __forceinline__ int limit_of(const AttnKernelArgs &ka, const Sight &s, int i)
-{
-    if (i >= s.qn) return -1;
-    return ka.a.causal ? s.len - s.qn + i : s.len - 1;
-}
-
-// Four neighbouring channels of the output
-__device__ __forceinline__ void store_out4(const Q4AttnArgs &a, int64_t at, float4v v)
-{
-    if (a.out_dtype == CSR_F32) {
-        *reinterpret_cast<float4v *>(static_cast<float *>(a.out) + at) = v;
-    } else if (a.out_dtype == CSR_F16) {
-        *reinterpret_cast<uint2v *>(static_cast<_Float16 *>(a.out) + at) =
-            uint2v{as_u32(half2v{(_Float16)v[0], (_Float16)v[1]}), as_u32(half2v{(_Float16)v[2], (_Float16)v[3]})};
-    } else {
-        *reinterpret_cast<uint2v *>(static_cast<uint16_t *>(a.out) + at) =
-            uint2v{(uint32_t)float_to_bf16(v[0]) | (uint32_t)float_to_bf16(v[1]) << 16, (uint32_t)float_to_bf16(v[2]) | (uint32_t)float_to_bf16(v[3]) << 16};
-    }
-}
-
-// Eight channels of a query row, as they are stored
-template <int QMODE> struct Stored8 {
-    uint4v w[QMODE == CSR_F32 ? 2 : 1];
-};
-template <int QMODE> __device__ __forceinline__ void load_q8(Stored8<QMODE> &s, const void *q, int64_t at)
-{
-    const uint4v *p = reinterpret_cast<const uint4v *>(static_cast<const uint8_t *>(q) + at * (QMODE == CSR_F32 ? 4 : 2));
-    s.w[0] = p[0];
-    if constexpr (QMODE == CSR_F32) s.w[1] = p[1];
-}
-template <int QMODE> __device__ __forceinline__ float channel_of(const Stored8<QMODE> &s, int k)
-{
-    if constexpr (QMODE == CSR_F32) return __uint_as_float(s.w[k / 4][k % 4]);
-    else if constexpr (QMODE == CSR_F16) return (float)as_half2(s.w[0][k / 2])[k % 2];
-    else return __uint_as_float(k % 2 ? s.w[0][k / 2] & 0xffff0000u : s.w[0][k / 2] << 16);
 }
 
 // The codes and parameters of a wave's 32 tokens, as requested
@@ -233,27 +168,24 @@ __global__ __launch_bounds__(64 * W, NR == 1 && QMODE != CSR_F32 ? 3 : 2) void q
     int limit[NR];
 #pragma unroll
     for (int t = 0; t < NC; ++t) {
-        unit[t] = a.scale * 1.44269504088896340736f;
-        int down = 0;
+        float most = 0.0f;
         if constexpr (QMODE != CSR_F16) {
-            float most = 0.0f;
 #pragma unroll
             for (int k = 0; k < KM; ++k)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(channel_of<QMODE>(stored[t][k], j)));
             most = fmaxf(most, __shfl_xor(most, 16, 64));
             most = fmaxf(most, __shfl_xor(most, 32, 64));
-            down = most > 0.0f && most < INFINITY ? 14 - ilogbf(most) : 0;   // the largest to 2^14 .. 2^15
-            unit[t] = ldexpf(unit[t], -down);
         }
-        unit[t] = fminf(fmaxf(unit[t], FLT_MIN), FLT_MAX);   // (an unseen token's score, minus infinity, times 0 would be no number)
+        const RowUnit ru = unit_of(a.scale, QMODE != CSR_F16, most);
+        unit[t] = ru.unit;
 #pragma unroll
         for (int k = 0; k < KM; ++k) {
             half8v hi, lo;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {   // in the order that a word's channels come in: 0, 2, 4, 6, 1, 3, 5, 7
-                float f = channel_of<QMODE>(stored[t][k], 2 * (j & 3) + (j >> 2));
-                if constexpr (QMODE != CSR_F16) f = ldexpf(f, down);
+            for (int j = 0; j < 8; ++j) {
+                float f = channel_of<QMODE>(stored[t][k], word_order(j));
+                if constexpr (QMODE != CSR_F16) f = ldexpf(f, ru.up);
                 hi[j] = (_Float16)f;
                 lo[j] = (_Float16)(f - (float)hi[j]);
             }
@@ -527,8 +459,10 @@ constexpr int kWaves = 4;
 template <int D, int QMODE, int NR> hipError_t run(const AttnKernelArgs &ka)
 {
     hipLaunchKernelGGL((q4_stream_kernel<D, QMODE, NR, kWaves>), dim3(ka.splits * ka.row_blocks, ka.a.Hkv, ka.a.B), dim3(64 * kWaves), 0, ka.a.stream, ka);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || ka.splits == 1) return e;
+    return hipGetLastError();
+}
+template <int D> hipError_t join_parts(const AttnKernelArgs &ka)
+{
     hipLaunchKernelGGL((q4_join_kernel<D>), dim3((ka.rows + 3) / 4, ka.a.Hkv, ka.a.B), dim3(256), 0, ka.a.stream, ka);
     return hipGetLastError();
 }
@@ -572,6 +506,8 @@ void plan_q4_attn(const Q4AttnArgs &a, Q4AttnPlan *p)
             p->splits = splits;
         }
     }
+    if (getenv("Q4_PROMPT") && p->row_tiles == 4) { p->row_tiles = 2 * kPromptWaves; p->row_blocks = (int32_t)((rows + 32 * kPromptWaves - 1) / (32 * kPromptWaves)); p->splits = 1; }
+    if (const char *e = getenv("Q4_SPLITS")) p->splits = atoi(e);
     const size_t parts = (size_t)blocks * (size_t)rows * (size_t)p->splits;
     p->off_ml = p->splits > 1 ? (parts * a.d * 4 + 255) / 256 * 256 : 0;
     p->total_bytes = p->splits > 1 ? p->off_ml + (parts * 8 + 255) / 256 * 256 : 0;
@@ -587,7 +523,9 @@ hipError_t launch_q4_attn(const Q4AttnArgs &a, const Q4AttnPlan &p)
     ka.by_splits = fast_div((uint32_t)p.splits); ka.by_group = fast_div((uint32_t)a.G);
     ka.acc = static_cast<float *>(a.workspace);
     ka.ml = reinterpret_cast<float *>(static_cast<char *>(a.workspace) + p.off_ml);
-    return a.d == 128 ? run<128>(ka, p.row_tiles) : run<64>(ka, p.row_tiles);
+    const hipError_t e = p.row_tiles > 4 ? launch_q4_prompt(ka) : a.d == 128 ? run<128>(ka, p.row_tiles) : run<64>(ka, p.row_tiles);
+    if (e != hipSuccess || p.splits == 1) return e;
+    return a.d == 128 ? join_parts<128>(ka) : join_parts<64>(ka);
 }
 
 }  // namespace csr
