@@ -16,7 +16,6 @@
 // Probabilities are relative to 2^13 below the running maximum (and the maximum is only moved when it is passed by 2^2), so that
 // as two fp16 - the value and what it lacks - they keep 22 bits down to 2^-27 of the largest, and the rest to 2^-37.
 #include <type_traits>
-#include <cstdlib>
 
 #include "q4_attn_common.h"
 
@@ -483,31 +482,37 @@ template <int D> hipError_t run(const AttnKernelArgs &ka, int row_tiles)
 
 }  // namespace
 
-// Parts of the token axis.  What a call takes is close to (us, fitted to 19 shapes of 8 to 512 (sequence, KV head) pairs and 128
-// to 8192 tokens, each at up to 10 numbers of parts)
-//   turns * (0.2 + 0.8 * c) * size    turns: of 128 tokens per workgroup, c: workgroups per CU, size: of a turn
-//   + 3.6 in one part; in more 6.7, 0.08 for every part beyond 16 and the parts' bytes at 4 TB/s, out and in.
+// The kernel for a call's query rows, and the parts of its token axis.  Up to 64 rows per KV head the waves of a workgroup share the
+// rows, 16, 32 or 64 of them, and divide the tokens; more (and fp16 or bf16 queries) go to the kernel whose waves share the tokens
+// and divide 256 rows.  Measured, us, with the rows in fours of 16 and with 256 at their best numbers of parts: 4 x 8 (sequences
+// x KV heads) of 4096 tokens, 64 rows, 25.8 and 24.2; 16 x 8 of 8192, 36 rows, 67 and 101; 4 x 8 of 8192, 128 rows, 56 and 38; 8 of
+// 10240, 8192 rows, 447 and 330.
+//   What a call takes is close to (us, fitted to 25 shapes at up to 10 numbers of parts each)
+//     turns * (0.2 + 0.8 c) * size   turns: of 128 tokens per workgroup, c: workgroups per CU, size: of a turn; for the many rows
+//     turns * c * size               turns of 64 tokens
+//     + 3.6 in one part; in more 6.7, 0.08 for every part beyond 16 and the parts' bytes at 4 TB/s, out and in.
 // Measured at 8 pairs of 517 tokens: 7.8 us in one part, 8.3 in three; of 8192: 56.4 in one, 13.5 in eight, 10.1 in 16, 10.6 in
 // 24; 512 pairs of 2048: 29.8 in one, 32.1 in two.
 void plan_q4_attn(const Q4AttnArgs &a, Q4AttnPlan *p)
 {
-    const int64_t rows = (int64_t)a.G * a.Tq, blocks = (int64_t)a.B * a.Hkv, step = kStep * kWaves;
-    p->row_tiles = rows <= 16 ? 1 : rows <= 32 || a.q_dtype == CSR_F32 ? 2 : 4;
-    p->row_blocks = (int32_t)((rows + 16 * p->row_tiles - 1) / (16 * p->row_tiles));
-    const float size = (a.d == 64 ? 0.6f : 1.0f) * (p->row_tiles == 1 ? 1.0f : p->row_tiles == 2 ? 1.36f : 2.6f);
+    const int64_t rows = (int64_t)a.G * a.Tq, blocks = (int64_t)a.B * a.Hkv;
+    const bool fp32 = a.q_dtype == CSR_F32, many = rows > 64 && !fp32;
+    p->row_tiles = many ? 2 * kPromptWaves : rows <= 16 ? 1 : rows <= 32 || fp32 ? 2 : 4;
+    const int64_t block_rows = 16 * p->row_tiles, step = many ? kPromptTile : kStep * kWaves;
+    p->row_blocks = (int32_t)((rows + block_rows - 1) / block_rows);
+    const float busy = (float)(rows < block_rows ? rows : block_rows) / block_rows;
+    const float size = (a.d == 64 ? 0.6f : 1.0f) * (many ? 0.75f + 1.45f * busy : p->row_tiles == 1 ? 1.0f : p->row_tiles == 2 ? 1.36f : 2.6f);
     float least = INFINITY;
     for (const int32_t splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 192, 256}) {
-        if (splits > 1 && splits > (a.T + step - 1) / step) break;
+        if (splits > 1 && splits > (a.T + 127) / 128) break;
         const int64_t turns = (a.T + step * splits - 1) / (step * splits), per_cu = (blocks * p->row_blocks * splits + kCus - 1) / kCus;
         const float join = splits == 1 ? 3.6f : 6.7f + 0.08f * (splits > 16 ? splits - 16 : 0) + (float)(blocks * rows * splits) * a.d * 8 / 4e6f;
-        const float cost = turns * (0.2f + 0.8f * per_cu) * size + join;
+        const float cost = turns * (many ? (float)per_cu : 0.2f + 0.8f * per_cu) * size + join;
         if (cost < least) {
             least = cost;
             p->splits = splits;
         }
     }
-    if (getenv("Q4_PROMPT") && p->row_tiles == 4) { p->row_tiles = 2 * kPromptWaves; p->row_blocks = (int32_t)((rows + 32 * kPromptWaves - 1) / (32 * kPromptWaves)); p->splits = 1; }
-    if (const char *e = getenv("Q4_SPLITS")) p->splits = atoi(e);
     const size_t parts = (size_t)blocks * (size_t)rows * (size_t)p->splits;
     p->off_ml = p->splits > 1 ? (parts * a.d * 4 + 255) / 256 * 256 : 0;
     p->total_bytes = p->splits > 1 ? p->off_ml + (parts * 8 + 255) / 256 * 256 : 0;

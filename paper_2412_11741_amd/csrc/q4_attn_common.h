@@ -12,6 +12,7 @@ namespace q4 {
 constexpr float kShift = 13.0f;    // p = 2^(score - maximum + kShift)
 constexpr float kSlack = 2.0f;     // a maximum may lag this far behind: p <= 2^15
 constexpr float kNone = -1e30f;    // a maximum before any token
+constexpr int kPromptTile = 64;    // tokens of a turn of the kernel for many rows
 constexpr int kPromptWaves = 8;    // of a workgroup of the kernel for many rows, 32 rows each
 
 struct AttnKernelArgs {

@@ -24,7 +24,7 @@ typedef float float16v __attribute__((ext_vector_type(16)));
 typedef short short4v __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) short4v lds_short4v;
 
-constexpr int kTile = 64;    // tokens
+constexpr int kTile = kPromptTile;
 constexpr int kRows = 32;    // query rows of a wave
 constexpr int kParts = 8;    // threads that share a token's key (value)
 
