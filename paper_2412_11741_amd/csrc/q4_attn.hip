@@ -404,10 +404,10 @@ __global__ __launch_bounds__(64 * W, NR == 1 && QMODE != CSR_F32 ? 3 : 2) void q
 }
 
 // Joins the parts of the token axis: a wave per query row, all its parts' requests ahead of their use
-template <int D>
+template <int D, int DEEP>   // DEEP: requests ahead
 __global__ __launch_bounds__(256) void q4_join_kernel(AttnKernelArgs ka)
 {
-    constexpr int LANES = D / 4, SIDE = 64 / LANES, DEEP = 8;   // of a part's row; parts side by side; requests ahead
+    constexpr int LANES = D / 4, SIDE = 64 / LANES;   // of a part's row; parts side by side
     const Q4AttnArgs &a = ka.a;
     const int lane = threadIdx.x & 63, b = blockIdx.z, h = blockIdx.y, bh = b * a.Hkv + h;
     const int r = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -462,7 +462,10 @@ template <int D, int QMODE, int NR> hipError_t run(const AttnKernelArgs &ka)
 }
 template <int D> hipError_t join_parts(const AttnKernelArgs &ka)
 {
-    hipLaunchKernelGGL((q4_join_kernel<D>), dim3((ka.rows + 3) / 4, ka.a.Hkv, ka.a.B), dim3(256), 0, ka.a.stream, ka);
+    const dim3 groups((ka.rows + 3) / 4, ka.a.Hkv, ka.a.B);
+    if (ka.splits * (D / 4) <= 128) hipLaunchKernelGGL((q4_join_kernel<D, 2>), groups, dim3(256), 0, ka.a.stream, ka);
+    else if (ka.splits * (D / 4) <= 256) hipLaunchKernelGGL((q4_join_kernel<D, 4>), groups, dim3(256), 0, ka.a.stream, ka);
+    else hipLaunchKernelGGL((q4_join_kernel<D, 8>), groups, dim3(256), 0, ka.a.stream, ka);
     return hipGetLastError();
 }
 template <int D, int QMODE> hipError_t run(const AttnKernelArgs &ka, int row_tiles)
