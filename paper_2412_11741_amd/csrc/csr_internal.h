@@ -192,6 +192,7 @@ struct Q4AttnPlan {
     int32_t row_tiles;   // tiles of 16 query rows (query token, head) that a workgroup takes
     int32_t row_blocks;  // workgroups along the query rows of a KV head
     int32_t splits;      // ... and along its tokens
+    bool alone;          // a workgroup has a CU to itself
     size_t off_ml, total_bytes;
 };
 void plan_q4_attn(const Q4AttnArgs &a, Q4AttnPlan *p);  // shape, types and causal of a

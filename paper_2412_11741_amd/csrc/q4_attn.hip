@@ -121,7 +121,7 @@ template <int D> __device__ __forceinline__ void request(Raw<D> &r, const Base &
 
 // QMODE: csr_dtype of q.  NR: tiles of 16 query rows.  W: waves.
 template <int D, int QMODE, int NR, int W>
-__global__ __launch_bounds__(64 * W, NR == 1 && QMODE != CSR_F32 ? 3 : 2) void q4_stream_kernel(AttnKernelArgs ka)
+__global__ __launch_bounds__(64 * W, NR == 1 && QMODE != CSR_F32 && W == 4 ? 3 : 2) void q4_stream_kernel(AttnKernelArgs ka)
 {
     constexpr int KM = D / 32;   // matrix instructions along a key's channels
     constexpr int UC = D / 16;   // channels of a lane's values
@@ -453,11 +453,11 @@ __global__ __launch_bounds__(256) void q4_join_kernel(AttnKernelArgs ka)
     store_out4(a, (int64_t)b * a.out_stride[0] + (int64_t)hq * a.out_stride[1] + (int64_t)i * a.out_stride[2] + ch, all == 0.0f ? float4v{} : value / all);
 }
 
-constexpr int kWaves = 4;
+constexpr int kWaves = 4, kAloneWaves = 8;   // of a workgroup; of one that has a CU to itself
 
-template <int D, int QMODE, int NR> hipError_t run(const AttnKernelArgs &ka)
+template <int D, int QMODE, int NR, int W = kWaves> hipError_t run(const AttnKernelArgs &ka)
 {
-    hipLaunchKernelGGL((q4_stream_kernel<D, QMODE, NR, kWaves>), dim3(ka.splits * ka.row_blocks, ka.a.Hkv, ka.a.B), dim3(64 * kWaves), 0, ka.a.stream, ka);
+    hipLaunchKernelGGL((q4_stream_kernel<D, QMODE, NR, W>), dim3(ka.splits * ka.row_blocks, ka.a.Hkv, ka.a.B), dim3(64 * W), 0, ka.a.stream, ka);
     return hipGetLastError();
 }
 template <int D> hipError_t join_parts(const AttnKernelArgs &ka)
@@ -468,18 +468,19 @@ template <int D> hipError_t join_parts(const AttnKernelArgs &ka)
     else hipLaunchKernelGGL((q4_join_kernel<D, 8>), groups, dim3(256), 0, ka.a.stream, ka);
     return hipGetLastError();
 }
-template <int D, int QMODE> hipError_t run(const AttnKernelArgs &ka, int row_tiles)
+template <int D, int QMODE> hipError_t run(const AttnKernelArgs &ka, int row_tiles, bool alone)
 {
+    if (alone) return run<D, QMODE, 1, kAloneWaves>(ka);
     if constexpr (QMODE != CSR_F32)
         if (row_tiles == 4) return run<D, QMODE, 4>(ka);
     return row_tiles == 1 ? run<D, QMODE, 1>(ka) : run<D, QMODE, 2>(ka);
 }
-template <int D> hipError_t run(const AttnKernelArgs &ka, int row_tiles)
+template <int D> hipError_t run(const AttnKernelArgs &ka, int row_tiles, bool alone)
 {
     switch (ka.a.q_dtype) {
-        case CSR_F32: return run<D, CSR_F32>(ka, row_tiles);
-        case CSR_F16: return run<D, CSR_F16>(ka, row_tiles);
-        default: return run<D, CSR_BF16>(ka, row_tiles);
+        case CSR_F32: return run<D, CSR_F32>(ka, row_tiles, alone);
+        case CSR_F16: return run<D, CSR_F16>(ka, row_tiles, alone);
+        default: return run<D, CSR_BF16>(ka, row_tiles, alone);
     }
 }
 
@@ -494,7 +495,7 @@ template <int D> hipError_t run(const AttnKernelArgs &ka, int row_tiles)
 //     turns * (0.2 + 0.8 c) * size   turns: of 128 tokens per workgroup, c: workgroups per CU, size: of a turn; for the many rows
 //     turns * c * size               turns of 64 tokens
 //     + 3.6 in one part; in more 6.7, 0.08 for every part beyond 16 and the parts' bytes at 4 TB/s, out and in.
-// Measured at 8 pairs of 517 tokens: 7.8 us in one part, 8.3 in three; of 8192: 56.4 in one, 13.5 in eight, 10.1 in 16, 10.6 in
+// Measured at 8 pairs of 517 tokens: 8.0 us in one part, 7.8 in three, 7.0 in one of eight waves; of 8192: 56.4 in one, 13.5 in eight, 10.1 in 16, 10.6 in
 // 24; 512 pairs of 2048: 29.8 in one, 32.1 in two.
 void plan_q4_attn(const Q4AttnArgs &a, Q4AttnPlan *p)
 {
@@ -516,6 +517,9 @@ void plan_q4_attn(const Q4AttnArgs &a, Q4AttnPlan *p)
             p->splits = splits;
         }
     }
+    // Short contexts of few pairs: eight waves, two of them to a SIMD, go through 256 tokens in 1.27 where four take 1.0 for 128.
+    p->alone = p->row_tiles == 1 && blocks <= kCus && (a.T + 255) / 256 * 1.27f * size + 3.6f < least;
+    if (p->alone) p->splits = 1;
     const size_t parts = (size_t)blocks * (size_t)rows * (size_t)p->splits;
     p->off_ml = p->splits > 1 ? (parts * a.d * 4 + 255) / 256 * 256 : 0;
     p->total_bytes = p->splits > 1 ? p->off_ml + (parts * 8 + 255) / 256 * 256 : 0;
@@ -531,7 +535,7 @@ hipError_t launch_q4_attn(const Q4AttnArgs &a, const Q4AttnPlan &p)
     ka.by_splits = fast_div((uint32_t)p.splits); ka.by_group = fast_div((uint32_t)a.G);
     ka.acc = static_cast<float *>(a.workspace);
     ka.ml = reinterpret_cast<float *>(static_cast<char *>(a.workspace) + p.off_ml);
-    const hipError_t e = p.row_tiles > 4 ? launch_q4_prompt(ka) : a.d == 128 ? run<128>(ka, p.row_tiles) : run<64>(ka, p.row_tiles);
+    const hipError_t e = p.row_tiles > 4 ? launch_q4_prompt(ka) : a.d == 128 ? run<128>(ka, p.row_tiles, p.alone) : run<64>(ka, p.row_tiles, p.alone);
     if (e != hipSuccess || p.splits == 1) return e;
     return a.d == 128 ? join_parts<128>(ka) : join_parts<64>(ka);
 }
