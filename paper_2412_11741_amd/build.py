@@ -66,7 +66,7 @@ def build_native(verbose: bool = False) -> str:
            "-D__HIP_PLATFORM_AMD__=1", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", INCLUDE,
            "-I", sysconfig.get_paths()["include"], "-isystem", os.path.join(top, "include"),
            "-isystem", os.path.join(top, "include", "torch", "csrc", "api", "include"), "-isystem", os.path.join(rocm, "include"),
-           NATIVE_SRC, "-o", NATIVE + ".tmp", "-L", os.path.join(top, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip"]
+           NATIVE_SRC, "-o", NATIVE + ".tmp", "-L", os.path.join(top, "lib"), "-ltorch_python", "-ltorch_cpu", "-ltorch_hip", "-lc10", "-lc10_hip"]
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.run(cmd, check=True)
