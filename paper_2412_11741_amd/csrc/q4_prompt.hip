@@ -52,7 +52,7 @@ __global__ __launch_bounds__(64 * W, 2) void q4_prompt_kernel(AttnKernelArgs ka,
     constexpr int CT = D / 32;          // tiles of output channels
     constexpr int WORDS = D / 8 / kParts, TOKENS = kTile * kParts / (64 * W);
     constexpr int BYTES = kTile * D * 2;
-    __shared__ __align__(16) uint8_t keys[2][BYTES], values[2][BYTES];
+    __shared__ __align__(16) uint8_t tiles[4 * BYTES];   // keys, keys, values, values
     __shared__ __align__(8) uint8_t bad[2][kTile][kParts];   // whose parameters are no finite numbers; of tiles that not all rows see
     const Q4AttnArgs &a = ka.a;
     // the workgroups of an XCD are neighbours: they read the same caches
@@ -111,8 +111,8 @@ __global__ __launch_bounds__(64 * W, 2) void q4_prompt_kernel(AttnKernelArgs ka,
                     *reinterpret_cast<uint4v *>(to) = uint4v{as_u32(fma2(whole2<false>(evens(c)), sc, m)), as_u32(fma2(whole2<true>(evens(c)), sc, m)),
                                                             as_u32(fma2(whole2<false>(odds(c)), sc, m)), as_u32(fma2(whole2<true>(odds(c)), sc, m))};
                 };
-                put(&keys[buffer][key_at<D>(t, part * WORDS + w)], raw.kc[i][w], ks, km);
-                put(&values[buffer][value_at<D>(t, part * WORDS + w)], raw.vc[i][w], vs, vm);
+                put(&tiles[buffer * BYTES + key_at<D>(t, part * WORDS + w)], raw.kc[i][w], ks, km);
+                put(&tiles[(2 + buffer) * BYTES + value_at<D>(t, part * WORDS + w)], raw.vc[i][w], vs, vm);
             }
         }
     };
@@ -150,6 +150,17 @@ __global__ __launch_bounds__(64 * W, 2) void q4_prompt_kernel(AttnKernelArgs ka,
     float top = kNone, sum = 0.0f;
     uint32_t poison = 0;   // parts of the channels that a token that is no number has reached
 
+    // where a lane reads: of token n channels 16 k + 8 hh .., and for the transposing read, where lane 16 e + 4 i + f reads channels
+    // 16 (e % 2) + 4 f .. of token 4 (e / 2) + i and gets four tokens of channel lane % 32.  What tokens, halves and steps add is
+    // constant: swizzles repeat after 16 tokens.  A tile's other buffer is one bit away.
+    static_assert((BYTES & (BYTES - 1)) == 0, "a power of two");
+    uint32_t key_from[KS], value_from[CT];
+#pragma unroll
+    for (int k = 0; k < KS; ++k) key_from[k] = key_at<D>(n, 2 * k + hh);
+#pragma unroll
+    for (int t = 0; t < CT; ++t)
+        value_from[t] = 2 * BYTES + value_at<D>(4 * hh + ((lane >> 2) & 3), 4 * t + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) + 8 * (lane & 1);
+
     if (begin < end) {
         convert(begin, 0);
         if (begin + kTile < end) request(begin + kTile);
@@ -173,7 +184,7 @@ __global__ __launch_bounds__(64 * W, 2) void q4_prompt_kernel(AttnKernelArgs ka,
                 float16v c = {};
 #pragma unroll
                 for (int k = 0; k < KS; ++k)
-                    c = mfma32(*reinterpret_cast<const half8v *>(&keys[buffer][key_at<D>(32 * u + n, 2 * k + hh)]), q[k], c);
+                    c = mfma32(*reinterpret_cast<const half8v *>(&tiles[key_from[k] + 32 * u * D * 2]), q[k], c);
                 if (some) {
 #pragma unroll
                     for (int j = 0; j < 16; ++j)
@@ -200,8 +211,6 @@ __global__ __launch_bounds__(64 * W, 2) void q4_prompt_kernel(AttnKernelArgs ka,
                     p[j >> 3][j & 7] = (_Float16)p0;
                     p[j >> 3][(j & 7) + 1] = (_Float16)p1;
                 }
-                // lane 16 e + 4 i + f reads channels 16 (e % 2) + 4 f .. of token 4 (e / 2) + i, and gets four tokens of channel lane % 32
-                const int token = 32 * u + 4 * (lane >> 5) + ((lane >> 2) & 3), run = 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1), rest = 8 * (lane & 1);
 #pragma unroll
                 for (int t = 0; t < CT; ++t)
 #pragma unroll
@@ -212,11 +221,15 @@ __global__ __launch_bounds__(64 * W, 2) void q4_prompt_kernel(AttnKernelArgs ka,
                         } v;
 #pragma unroll
                         for (int e = 0; e < 2; ++e)
-                            v.s[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4v *)&values[buffer][value_at<D>(token + 16 * k + 8 * e, 4 * t + run) + rest]);
+                            v.s[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4v *)&tiles[value_from[t] + (32 * u + 16 * k + 8 * e) * D * 2]);
                         o[t] = mfma32(v.h, p[k], o[t]);
                     }
             }
         }
+#pragma unroll
+        for (int k = 0; k < KS; ++k) key_from[k] ^= BYTES;
+#pragma unroll
+        for (int t = 0; t < CT; ++t) value_from[t] ^= BYTES;
         __syncthreads();
     }
     if (!busy) return;
