@@ -30,6 +30,10 @@ constexpr int kParts = 8;    // threads that share a token's key (value)
 
 __device__ __forceinline__ float16v mfma32(half8v a, half8v b, float16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 
+__device__ __forceinline__ half8v join(half2v a, half2v b, half2v c, half2v d) { return half8v{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]}; }
+// sum + p[0] + p[1]
+__device__ __forceinline__ float dot2(half2v p, float sum) { return __builtin_amdgcn_fdot2(p, half2v{(_Float16)1.0f, (_Float16)1.0f}, sum, false); }
+
 // Where 16 bytes (eight channels) of a token's row lie in a tile, in bytes
 template <int D> __device__ __forceinline__ int key_at(int token, int chunk)
 {
@@ -46,7 +50,7 @@ template <int WORDS, int TOKENS> struct RawTile {
 };
 
 template <int D, int QMODE, int W>
-__global__ __launch_bounds__(64 * W, 2) void q4_prompt_kernel(AttnKernelArgs ka, int total)
+__global__ __launch_bounds__(64 * W, D == 64 ? 4 : 2) void q4_prompt_kernel(AttnKernelArgs ka, int total)
 {
     constexpr int KS = D / 16;          // steps of the products along channels
     constexpr int CT = D / 32;          // tiles of output channels
@@ -179,52 +183,60 @@ __global__ __launch_bounds__(64 * W, 2) void q4_prompt_kernel(AttnKernelArgs ka,
                     if (tb + t <= limit)
                         for (int p = 0; p < kParts; ++p) poison |= (uint32_t)(bad[buffer][t][p] != 0) << p;
             }
+            float16v c[2] = {};   // 32 tokens each
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {   // 32 tokens
-                float16v c = {};
+            for (int k = 0; k < KS; ++k)
 #pragma unroll
-                for (int k = 0; k < KS; ++k)
-                    c = mfma32(*reinterpret_cast<const half8v *>(&tiles[key_from[k] + 32 * u * D * 2]), q[k], c);
-                if (some) {
+                for (int u = 0; u < 2; ++u)
+                    c[u] = mfma32(*reinterpret_cast<const half8v *>(&tiles[key_from[k] + 32 * u * D * 2]), q[k], c[u]);
+            if (some) {
 #pragma unroll
-                    for (int j = 0; j < 16; ++j)
-                        if (tb + 32 * u + 8 * (j >> 2) + 4 * hh + (j & 3) > limit) c[j] = -INFINITY;
-                }
-                float best = c[0];
-#pragma unroll
-                for (int j = 1; j < 16; ++j) best = fmaxf(best, c[j]);
-                best *= unit;
-                if (__any(best > top + kSlack)) {
-                    best = fmaxf(fmaxf(best, __shfl_xor(best, 32, 64)), top);
-                    const float fade = __builtin_amdgcn_exp2f(top - best);
-                    top = best;
-                    sum *= fade;
-#pragma unroll
-                    for (int t = 0; t < CT; ++t) o[t] *= fade;
-                }
-                const float lift = kShift - top;
-                half8v p[2];
-#pragma unroll
-                for (int j = 0; j < 16; j += 2) {
-                    const float p0 = __builtin_amdgcn_exp2f(fmaf(c[j], unit, lift)), p1 = __builtin_amdgcn_exp2f(fmaf(c[j + 1], unit, lift));
-                    sum += p0 + p1;
-                    p[j >> 3][j & 7] = (_Float16)p0;
-                    p[j >> 3][(j & 7) + 1] = (_Float16)p1;
-                }
-#pragma unroll
-                for (int t = 0; t < CT; ++t)
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        union {
-                            short4v s[2];
-                            half8v h;
-                        } v;
-#pragma unroll
-                        for (int e = 0; e < 2; ++e)
-                            v.s[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4v *)&tiles[value_from[t] + (32 * u + 16 * k + 8 * e) * D * 2]);
-                        o[t] = mfma32(v.h, p[k], o[t]);
-                    }
+                for (int j = 0; j < 32; ++j)
+                    if (tb + 8 * (j >> 2) + 4 * hh + (j & 3) > limit) c[j >> 4][j & 15] = -INFINITY;
             }
+            // probabilities against the maximum as it is; their sum tells whether one of them has left fp16's range - 32 of up to
+            // 2^14 are no reason - and the maximum has to be moved first
+            half2v p[16];
+            float part_sum;
+            const auto weigh = [&]() {
+                const float lift = kShift - top;
+                part_sum = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const float16v &x = c[j >> 3];
+                    const int e = 2 * (j & 7);
+                    p[j] = half2v{(_Float16)__builtin_amdgcn_exp2f(fmaf(x[e], unit, lift)), (_Float16)__builtin_amdgcn_exp2f(fmaf(x[e + 1], unit, lift))};
+                    part_sum = dot2(p[j], part_sum);
+                }
+            };
+            weigh();
+            if (__any(part_sum > 32.0f * 16384.0f)) {
+                float best = c[0][0];
+#pragma unroll
+                for (int j = 1; j < 32; ++j) best = fmaxf(best, c[j >> 4][j & 15]);
+                best *= unit;
+                best = fmaxf(fmaxf(best, __shfl_xor(best, 32, 64)), top);
+                const float fade = __builtin_amdgcn_exp2f(top - best);
+                top = best;
+                sum *= fade;
+#pragma unroll
+                for (int t = 0; t < CT; ++t) o[t] *= fade;
+                weigh();
+            }
+            sum += part_sum;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)   // 16 tokens each
+#pragma unroll
+                for (int t = 0; t < CT; ++t) {
+                    union {
+                        short4v s[2];
+                        half8v h;
+                    } v;
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                        v.s[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4v *)&tiles[value_from[t] + (16 * k + 8 * e) * D * 2]);
+                    o[t] = mfma32(v.h, join(p[4 * k], p[4 * k + 1], p[4 * k + 2], p[4 * k + 3]), o[t]);
+                }
         }
 #pragma unroll
         for (int k = 0; k < KS; ++k) key_from[k] ^= BYTES;
