@@ -333,7 +333,7 @@ csr_status csr_check_codes(const void *idx, int32_t idx_dtype, int64_t count, in
 typedef struct {
     int32_t B;          /* sequences; >= 0                                                  */
     int32_t Hkv;        /* KV heads                                                         */
-    int64_t n;          /* rows of X / out per (b, h); >= 0                                 */
+    int64_t n;          /* rows of X / out per (b, h); 0 .. 2^26                            */
     int64_t T;          /* rows allocated per (b, h) in the cache; 0 .. 2^20                */
     int32_t d;          /* head dimension: 64 or 128                                        */
     int32_t group;      /* channels per scale: 32, 64 or 128, at most d                     */

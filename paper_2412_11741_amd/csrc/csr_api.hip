@@ -302,8 +302,8 @@ csr_status check_q4_rows(const char *call, const csr_q4_rows_desc *d, bool reads
         return fail(CSR_ERR_UNSUPPORTED, "%s: d=%d must be 64 or 128, group=%d 32, 64 or 128 and at most d", call, d->d, d->group);
     if (d->T > (int64_t)1 << 20) return fail(CSR_ERR_UNSUPPORTED, "%s: T above 2^20", call);
     if (d->pos0 > (int64_t)1 << 40 || d->pos0 < -((int64_t)1 << 40)) return fail(CSR_ERR_INVALID_ARG, "%s: pos0 outside +-2^40", call);
-    if (d->n > 0x3fffffff || (d->B > 0 && (int64_t)d->B * d->Hkv > 0x3fffffff / (d->n > 0 ? d->n : 1)))
-        return fail(CSR_ERR_UNSUPPORTED, "%s: more than 2^30 rows in one call", call);
+    if (d->n > 1 << 26 || (int64_t)d->B * d->Hkv > 0x7fffffff)
+        return fail(CSR_ERR_UNSUPPORTED, "%s: n above 2^26, or B * Hkv above 2^31 - 1", call);
     const int64_t size[3] = {d->B, d->Hkv, d->n}, xs[3] = {d->x_stride_b, d->x_stride_h, d->x_stride_t},
                   os[3] = {d->out_stride_b, d->out_stride_h, d->out_stride_t};
     csr_status st = reads_x ? check_q4_strides(call, "X", xs, size, d->x_dtype, d->d, false) : CSR_OK;

@@ -43,7 +43,8 @@ struct RowsKernelArgs {
     const int32_t *pos, *counts;
     int64_t pos0;
     FastDiv by_tiles, by_h;   // by_tiles: tokens (FLAT) or workgroups (else) per sequence and head
-    uint32_t n, T, total;     // total: vectors of a side
+    uint32_t n, T, total;     // total: vectors of a side in this launch
+    uint32_t first_block;     // (sequence, head) of the launch's first
 };
 
 template <typename P> __device__ __forceinline__ P uniform(P p)
@@ -67,7 +68,8 @@ template <int MODE, int LOGW, int LOGC> __device__ __forceinline__ bool place_of
     constexpr uint32_t PER = 256u >> LOGW;
     const uint32_t mine = threadIdx.x >> LOGW, v = MODE == FLAT ? blockIdx.x * PER + mine : blockIdx.x;
     if (MODE == FLAT && v >= a.total) return false;
-    const uint32_t bh = quotient(v, a.by_tiles), first = MODE == FLAT ? v - bh * a.by_tiles.div : (v - bh * a.by_tiles.div) * PER;
+    const uint32_t nth = quotient(v, a.by_tiles), first = MODE == FLAT ? v - nth * a.by_tiles.div : (v - nth * a.by_tiles.div) * PER;
+    const uint32_t bh = a.first_block + nth;
     const uint32_t h = bh - quotient(bh, a.by_h) * a.by_h.div;
     p.b = quotient(bh, a.by_h);
     p.t = MODE == FLAT ? first : first + mine;
@@ -84,7 +86,7 @@ template <int MODE, int LOGW, int LOGC> __device__ __forceinline__ bool place_of
     }
     return true;
 }
-// Its row of the cache; false for none.  (A first row beyond 32 bits is out of reach of 2^30 tokens and 2^20 rows.)
+// Its row of the cache; false for none.  (A first row beyond 32 bits is out of reach of 2^26 tokens and 2^20 rows.)
 __device__ __forceinline__ bool row_of(const RowsKernelArgs &a, const Place &p, uint32_t &row)
 {
     const int64_t row0 = a.pos0 + (a.pos ? (int64_t)a.pos[p.b] : 0);
@@ -325,45 +327,46 @@ __global__ __launch_bounds__(256) void q4_read_kernel(RowsKernelArgs a)
 }
 
 // A workgroup of one sequence and head from half a workgroup's vectors on; fewer share one.
-struct RowsLaunch {
-    RowsKernelArgs a;
-    int mode;
-    dim3 groups;
-};
-RowsLaunch rows_launch(const Q4RowsArgs &r, int sides, int log_threads)
+// A launch takes 2^20 workgroups' worth of (sequence, head) blocks (the runtime's limit is 2^32 threads).
+constexpr uint32_t kMostGroups = 1u << 20;
+
+template <typename K> hipError_t launch(const Q4RowsArgs &r, int sides, int log_threads, K flat, K near, K past)
 {
-    RowsLaunch l{};
-    RowsKernelArgs &a = l.a;
+    RowsKernelArgs a{};
     const uint32_t per = 256u >> log_threads, blocks = (uint32_t)r.B * (uint32_t)r.Hkv;
     const int64_t xe = r.x_dtype == CSR_F32 ? 4 : 2, oe = r.out_dtype == CSR_F32 ? 4 : 2;
-    bool flat = r.n < per / 2;
+    bool any = r.n < per / 2;
     for (int k = 0; k < sides; ++k) {
         const Q4RowsSide &s = r.side[k];
         a.side[k] = {static_cast<const uint8_t *>(s.x), static_cast<uint32_t *>(s.codes), static_cast<uint32_t *>(s.params), static_cast<uint8_t *>(s.out),
                      s.x_stride[0] * xe, s.x_stride[1] * xe, s.x_stride[2] * xe, s.out_stride[0] * oe, s.out_stride[1] * oe, s.out_stride[2] * oe,
                      s.group == 32 ? 5 : s.group == 64 ? 6 : 7};
-        if (a.side[k].xt > (1 << 26) || a.side[k].ot > (1 << 26)) flat = true;   // (31 of them are 2^31 bytes)
+        if (a.side[k].xt > (1 << 26) || a.side[k].ot > (1 << 26)) any = true;   // (31 of them are 2^31 bytes)
     }
+    const bool stream = a.side[0].out && (int64_t)sides * blocks * r.n * r.d * oe >= kStreamBytes;
+    const K kernel = any ? flat : stream ? past : near;
     a.pos = r.pos; a.counts = r.counts; a.pos0 = r.pos0;
     a.n = (uint32_t)r.n; a.T = (uint32_t)r.T;
-    a.total = blocks * a.n;
-    l.mode = flat ? FLAT : a.side[0].out && (int64_t)sides * a.total * r.d * oe >= kStreamBytes ? PAST : NEAR;
-    const uint32_t tiles = flat ? a.n : (a.n + per - 1) / per;
+    const uint32_t tiles = any ? a.n : (a.n + per - 1) / per;
     a.by_tiles = fast_div(tiles); a.by_h = fast_div((uint32_t)r.Hkv);
-    l.groups = dim3(flat ? (a.total + per - 1) / per : blocks * tiles, sides);
-    return l;
+    const uint64_t fit = (uint64_t)kMostGroups * (any ? per : 1) / tiles;
+    const uint32_t step = fit < 1 ? 1 : fit < blocks ? (uint32_t)fit : blocks;
+    for (uint32_t b = 0; b < blocks; b += step) {
+        const uint32_t now = blocks - b < step ? blocks - b : step;
+        a.first_block = b;
+        a.total = now * a.n;
+        hipLaunchKernelGGL(kernel, dim3(any ? (a.total + per - 1) / per : now * tiles, sides), dim3(256), 0, r.stream, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
-
-template <typename K> K pick(int mode, K flat, K near, K past) { return mode == FLAT ? flat : mode == NEAR ? near : past; }
 
 template <int DT, int OUT> hipError_t write(const Q4RowsArgs &r, int sides)
 {
     constexpr int kPast = OUT >= 0 ? PAST : NEAR;
-    const RowsLaunch l = rows_launch(r, sides, r.d == 128 ? 4 : 3);
-    const auto kernel = r.d == 128 ? pick(l.mode, q4_write_kernel<DT, OUT, 4, FLAT>, q4_write_kernel<DT, OUT, 4, NEAR>, q4_write_kernel<DT, OUT, 4, kPast>)
-                                   : pick(l.mode, q4_write_kernel<DT, OUT, 3, FLAT>, q4_write_kernel<DT, OUT, 3, NEAR>, q4_write_kernel<DT, OUT, 3, kPast>);
-    hipLaunchKernelGGL(kernel, l.groups, dim3(256), 0, r.stream, l.a);
-    return hipGetLastError();
+    return r.d == 128 ? launch(r, sides, 4, q4_write_kernel<DT, OUT, 4, FLAT>, q4_write_kernel<DT, OUT, 4, NEAR>, q4_write_kernel<DT, OUT, 4, kPast>)
+                      : launch(r, sides, 3, q4_write_kernel<DT, OUT, 3, FLAT>, q4_write_kernel<DT, OUT, 3, NEAR>, q4_write_kernel<DT, OUT, 3, kPast>);
 }
 template <int DT> hipError_t write(const Q4RowsArgs &r, int sides)
 {
@@ -376,12 +379,9 @@ template <int DT> hipError_t write(const Q4RowsArgs &r, int sides)
 }
 template <int OUT> hipError_t read(const Q4RowsArgs &r)
 {
-    constexpr int MORE = OUT == CSR_F32 ? 1 : 0;
-    const RowsLaunch l = rows_launch(r, 1, (r.d == 128 ? 4 : 3) + MORE);
-    const auto kernel = r.d == 128 ? pick(l.mode, q4_read_kernel<OUT, 4 + MORE, FLAT>, q4_read_kernel<OUT, 4 + MORE, NEAR>, q4_read_kernel<OUT, 4 + MORE, PAST>)
-                                   : pick(l.mode, q4_read_kernel<OUT, 3 + MORE, FLAT>, q4_read_kernel<OUT, 3 + MORE, NEAR>, q4_read_kernel<OUT, 3 + MORE, PAST>);
-    hipLaunchKernelGGL(kernel, l.groups, dim3(256), 0, r.stream, l.a);
-    return hipGetLastError();
+    constexpr int W = OUT == CSR_F32 ? 5 : 4;   // log2 of the threads of a vector of 128
+    return r.d == 128 ? launch(r, 1, W, q4_read_kernel<OUT, W, FLAT>, q4_read_kernel<OUT, W, NEAR>, q4_read_kernel<OUT, W, PAST>)
+                      : launch(r, 1, W - 1, q4_read_kernel<OUT, W - 1, FLAT>, q4_read_kernel<OUT, W - 1, NEAR>, q4_read_kernel<OUT, W - 1, PAST>);
 }
 
 }  // namespace

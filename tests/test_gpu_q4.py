@@ -523,3 +523,17 @@ def test_refusals_name_the_mistake():
     bad = csr.csr_q4_alloc(1, 1, 4, 64, 64)
     with pytest.raises(csr.CsrError, match="group"):             # four groups of 16
         csr.csr_q4_read(bad[0], torch.zeros(1, 1, 4, 4, 2, dtype=F16, device="cuda"))
+
+
+def test_more_blocks_than_one_launch_takes():
+    # 600000 (sequence, head) blocks: rows in two launches; the first, the last and those around the cut
+    B, Hkv, n, d = 12, 50000, 64, 64
+    X = torch.randn(1, 50, n, d, device="cuda", generator=_gen(200)).to(F16).repeat(B, Hkv // 50, 1, 1)
+    X[3:] += 1.0
+    codes, params = csr.csr_q4_alloc(B, Hkv, n, d, 64)
+    vals = csr.csr_q4_write(X, codes, params, values=True)
+    assert torch.equal(vals, csr.csr_q4_read(codes, params))
+    for b, h in ((0, 0), (0, 49999), (10, 24287), (10, 24288), (10, 24289), (11, 49999)):   # 524288 blocks a launch
+        want = ref.quantise(_np(X[b, h]), 64)
+        assert (codes[b, h].cpu().numpy() == want[0]).all() and _same(params[b, h].cpu().numpy(), want[1]).all()
+    assert torch.equal(vals[:3, :50], vals[:3, 50:100]) and torch.equal(vals[4:, :50], vals[4:, 49950:])

@@ -75,7 +75,7 @@ BAD_ROWS = [
     (dict(Hkv=0), B.CSR_ERR_INVALID_ARG), (dict(flags=1), B.CSR_ERR_INVALID_ARG), (dict(out_dtype=3), B.CSR_ERR_INVALID_ARG),
     (dict(d=96), B.CSR_ERR_UNSUPPORTED), (dict(d=256), B.CSR_ERR_UNSUPPORTED), (dict(group=16), B.CSR_ERR_UNSUPPORTED),
     (dict(d=64, group=128), B.CSR_ERR_UNSUPPORTED), (dict(group=96), B.CSR_ERR_UNSUPPORTED), (dict(T=(1 << 20) + 1), B.CSR_ERR_UNSUPPORTED),
-    (dict(pos0=1 << 41), B.CSR_ERR_INVALID_ARG), (dict(n=1 << 29), B.CSR_ERR_UNSUPPORTED),
+    (dict(pos0=1 << 41), B.CSR_ERR_INVALID_ARG), (dict(n=(1 << 26) + 1), B.CSR_ERR_UNSUPPORTED), (dict(B=1 << 20, Hkv=1 << 11), B.CSR_ERR_UNSUPPORTED),
     (dict(out_stride_t=64), B.CSR_ERR_INVALID_ARG), (dict(out_stride_h=644), B.CSR_ERR_INVALID_ARG), (dict(out_stride_b=-1280), B.CSR_ERR_INVALID_ARG),
     (dict(out_stride_b=1 << 48), B.CSR_ERR_UNSUPPORTED),
 ]
