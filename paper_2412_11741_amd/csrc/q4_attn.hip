@@ -13,8 +13,8 @@
 //   - a lane's four scores of either half of the 32 tokens are tokens 8 kg .. 8 kg + 7 and go into the next product as they are;
 //   - lane (m, kg) takes channels (d / 16) m .. of the values of tokens 8 kg .. 8 kg + 7: two tokens' words are cut into halves and
 //     joined, and every pair of codes is then one channel of two tokens.
-// Probabilities are relative to 2^13 below the running maximum (and the maximum is only moved when it is passed by 2^2), so that
-// as two fp16 - the value and what it lacks - they keep 22 bits down to 2^-27 of the largest, and the rest to 2^-37.
+// Probabilities are relative to 2^12 below the running maximum, which is moved when a lane's eight add up to more than an fp16
+// holds: as two fp16 - the value and what it lacks - they keep 22 bits down to 2^-26 of the largest, and the rest to 2^-36.
 #include <type_traits>
 
 #include "q4_attn_common.h"
@@ -27,11 +27,6 @@ using namespace q4;
 constexpr int kStep = 32;          // tokens of a wave's turn
 
 __device__ __forceinline__ float4v mfma(half8v a, half8v b, float4v c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
-
-__device__ __forceinline__ half8v join(half2v a, half2v b, half2v c, half2v d)
-{
-    return half8v{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-}
 
 // p less the fp16 in the low (high) half of a word, exactly
 __device__ __forceinline__ float less_low(float p, uint32_t h)
@@ -126,7 +121,8 @@ __global__ __launch_bounds__(64 * W, NR == 1 && QMODE != CSR_F32 && W == 4 ? 3 :
     constexpr int KM = D / 32;   // matrix instructions along a key's channels
     constexpr int UC = D / 16;   // channels of a lane's values
     constexpr bool kTwo = QMODE == CSR_F32;
-    constexpr bool kMany = NR == 4;        // queries wait in LDS, probabilities are one fp16
+    constexpr bool kMany = NR == 4;        // queries wait in LDS
+    constexpr bool kOneP = NR > 1 && !kTwo;   // probabilities are one fp16: the second would be a third of the matrix instructions
     constexpr bool kOneSet = kMany || (kTwo && NR == 2);   // of registers for requests: two do not fit
     static_assert(!kMany || (W == 4 && !kTwo), "a wave converts one tile of queries");
     const Q4AttnArgs &a = ka.a;
@@ -210,6 +206,7 @@ __global__ __launch_bounds__(64 * W, NR == 1 && QMODE != CSR_F32 && W == 4 ? 3 :
 #pragma unroll
     for (int t = 0; t < NR; ++t) { top[t] = kNone; sum[t] = 0.0f; }
 
+    bool first = true;
     const auto turn = [&](Raw<D> &r) __attribute__((always_inline)) {
         half8v k8[2][KM];
 #pragma unroll
@@ -273,14 +270,47 @@ __global__ __launch_bounds__(64 * W, NR == 1 && QMODE != CSR_F32 && W == 4 ? 3 :
                 }
             }
         }
-        half8v ph[NR], pl[kMany ? 1 : NR];
+        // Probabilities against the maxima as they are.  A lane's sum of eight tells whether one of them may have left fp16's range; the
+        // maxima are moved first then, and in a wave's first turn.
+        half8v ph[NR], pl[kOneP ? 1 : NR];
+        float part_sum[NR];
+        const auto weigh = [&](int t) __attribute__((always_inline)) {
+            const float lift = kShift - top[t];
+            half2v p2[4], rest[4];
+            part_sum[t] = 0.0f;
 #pragma unroll
-        for (int t = 0; t < NR; ++t) {
-            float best = score[t][0];
+            for (int j = 0; j < 4; ++j) {
+                const float p0 = __builtin_amdgcn_exp2f(fmaf(score[t][2 * j], unit[t], lift));
+                const float p1 = __builtin_amdgcn_exp2f(fmaf(score[t][2 * j + 1], unit[t], lift));
+                p2[j] = half2v{(_Float16)p0, (_Float16)p1};
+                if constexpr (kOneP) {
+                    part_sum[t] = dot2(p2[j], part_sum[t]);
+                } else {
+                    part_sum[t] += p0 + p1;
+                    rest[j] = half2v{(_Float16)less_low(p0, as_u32(p2[j])), (_Float16)less_high(p1, as_u32(p2[j]))};
+                }
+            }
+            ph[t] = join(p2[0], p2[1], p2[2], p2[3]);
+            if constexpr (!kOneP) pl[t] = join(rest[0], rest[1], rest[2], rest[3]);
+        };
+        bool moved = first;
+        if (!first) {
+            float largest = 0.0f;
 #pragma unroll
-            for (int j = 1; j < 8; ++j) best = fmaxf(best, score[t][j]);
-            best *= unit[t];
-            if (__any(best > top[t] + kSlack)) {
+            for (int t = 0; t < NR; ++t) {
+                weigh(t);
+                largest = fmaxf(largest, part_sum[t]);
+            }
+            moved = __any(largest > kMostHalf);
+        }
+        if (moved) {
+            first = false;
+#pragma unroll
+            for (int t = 0; t < NR; ++t) {
+                float best = score[t][0];
+#pragma unroll
+                for (int j = 1; j < 8; ++j) best = fmaxf(best, score[t][j]);
+                best *= unit[t];
                 best = fmaxf(best, __shfl_xor(best, 16, 64));
                 best = fmaxf(best, __shfl_xor(best, 32, 64));
                 best = fmaxf(best, top[t]);
@@ -289,20 +319,11 @@ __global__ __launch_bounds__(64 * W, NR == 1 && QMODE != CSR_F32 && W == 4 ? 3 :
                 sum[t] *= fade;
 #pragma unroll
                 for (int c = 0; c < UC; ++c) o[t][c] *= fade;
+                weigh(t);
             }
-            const float lift = kShift - top[t];
-            half2v p2[4], rest[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float p0 = __builtin_amdgcn_exp2f(fmaf(score[t][2 * j], unit[t], lift));
-                const float p1 = __builtin_amdgcn_exp2f(fmaf(score[t][2 * j + 1], unit[t], lift));
-                sum[t] += p0 + p1;
-                p2[j] = half2v{(_Float16)p0, (_Float16)p1};
-                if constexpr (!kMany) rest[j] = half2v{(_Float16)less_low(p0, as_u32(p2[j])), (_Float16)less_high(p1, as_u32(p2[j]))};
-            }
-            ph[t] = join(p2[0], p2[1], p2[2], p2[3]);
-            if constexpr (!kMany) pl[t] = join(rest[0], rest[1], rest[2], rest[3]);
         }
+#pragma unroll
+        for (int t = 0; t < NR; ++t) sum[t] += part_sum[t];
         half2v vs[4], vm[4];
         uint32_t low[4], high[4];   // channels 0 .. 3 and 4 .. 7 of two tokens
 #pragma unroll
@@ -325,7 +346,7 @@ __global__ __launch_bounds__(64 * W, NR == 1 && QMODE != CSR_F32 && W == 4 ? 3 :
 #pragma unroll
             for (int t = 0; t < NR; ++t) {
                 o[t][C] = mfma(v8, ph[t], o[t][C]);
-                if constexpr (!kMany) o[t][C] = mfma(v8, pl[t], o[t][C]);
+                if constexpr (!kOneP) o[t][C] = mfma(v8, pl[t], o[t][C]);
             }
         };
         channel(std::integral_constant<int, 0>{});

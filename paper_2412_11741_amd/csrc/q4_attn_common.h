@@ -9,8 +9,8 @@
 namespace csr {
 namespace q4 {
 
-constexpr float kShift = 13.0f;    // p = 2^(score - maximum + kShift)
-constexpr float kSlack = 2.0f;     // a maximum may lag this far behind: p <= 2^15
+constexpr float kShift = 12.0f;         // p = 2^(score - maximum + kShift)
+constexpr float kMostHalf = 65504.0f;   // the largest fp16
 constexpr float kNone = -1e30f;    // a maximum before any token
 constexpr int kPromptTile = 64;    // tokens of a turn of the kernel for many rows
 constexpr int kPromptWaves = 8;    // of a workgroup of the kernel for many rows, 32 rows each
@@ -75,6 +75,10 @@ template <int QMODE> __device__ __forceinline__ float channel_of(const Stored8<Q
     else if constexpr (QMODE == CSR_F16) return (float)as_half2(s.w[0][k / 2])[k % 2];
     else return __uint_as_float(k % 2 ? s.w[0][k / 2] & 0xffff0000u : s.w[0][k / 2] << 16);
 }
+
+__device__ __forceinline__ half8v join(half2v a, half2v b, half2v c, half2v d) { return half8v{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]}; }
+// sum + p[0] + p[1]
+__device__ __forceinline__ float dot2(half2v p, float sum) { return __builtin_amdgcn_fdot2(p, half2v{(_Float16)1.0f, (_Float16)1.0f}, sum, false); }
 
 // The factor of a row's scores, in powers of two, and the power of two that its channels are multiplied by before they become
 // fp16: none for fp16, else what brings the largest to 2^14 .. 2^15.

@@ -30,10 +30,6 @@ constexpr int kParts = 8;    // threads that share a token's key (value)
 
 __device__ __forceinline__ float16v mfma32(half8v a, half8v b, float16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 
-__device__ __forceinline__ half8v join(half2v a, half2v b, half2v c, half2v d) { return half8v{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]}; }
-// sum + p[0] + p[1]
-__device__ __forceinline__ float dot2(half2v p, float sum) { return __builtin_amdgcn_fdot2(p, half2v{(_Float16)1.0f, (_Float16)1.0f}, sum, false); }
-
 // Where 16 bytes (eight channels) of a token's row lie in a tile, in bytes
 template <int D> __device__ __forceinline__ int key_at(int token, int chunk)
 {
@@ -194,8 +190,8 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 4 : 2) void q4_prompt_kernel(Attn
                 for (int j = 0; j < 32; ++j)
                     if (tb + 8 * (j >> 2) + 4 * hh + (j & 3) > limit) c[j >> 4][j & 15] = -INFINITY;
             }
-            // probabilities against the maximum as it is; their sum tells whether one of them has left fp16's range - 32 of up to
-            // 2^14 are no reason - and the maximum has to be moved first
+            // probabilities against the maximum as it is; the sum of them as fp16 is infinite where one has left their range, and is
+            // held to 32 of 2^13: the maximum is moved first then
             half2v p[16];
             float part_sum;
             const auto weigh = [&]() {
@@ -210,7 +206,7 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 4 : 2) void q4_prompt_kernel(Attn
                 }
             };
             weigh();
-            if (__any(part_sum > 32.0f * 16384.0f)) {
+            if (__any(part_sum > 32.0f * 8192.0f)) {
                 float best = c[0][0];
 #pragma unroll
                 for (int j = 1; j < 32; ++j) best = fmaxf(best, c[j >> 4][j & 15]);
