@@ -122,7 +122,8 @@ __global__ __launch_bounds__(64 * W, NR == 1 && QMODE != CSR_F32 && W == 4 ? 3 :
     constexpr int UC = D / 16;   // channels of a lane's values
     constexpr bool kTwo = QMODE == CSR_F32;
     constexpr bool kMany = NR == 4;        // queries wait in LDS
-    constexpr bool kOneP = NR > 1 && !kTwo;   // probabilities are one fp16: the second would be a third of the matrix instructions
+    // probabilities are one fp16, where the second would be a third of the matrix instructions or the queries are rounded to 2^-8
+    constexpr bool kOneP = !kTwo && (NR > 1 || QMODE == CSR_BF16);
     constexpr bool kOneSet = kMany || (kTwo && NR == 2);   // of registers for requests: two do not fit
     static_assert(!kMany || (W == 4 && !kTwo), "a wave converts one tile of queries");
     const Q4AttnArgs &a = ka.a;

@@ -212,7 +212,7 @@ def _check(q, cache, got, seq_lens=None, q_lens=None, causal=True, scale=0.0):
     lens = [T] * B if seq_lens is None else [max(0, min(int(n), T)) for n in seq_lens]
     qn = [Tq] * B if q_lens is None else [max(0, min(int(n), Tq)) for n in q_lens]
     want, spread, size = ref.attention(_np(q4), k, v, lens, qn, scale or d ** -0.5, causal)
-    one_p = Tq * (Hq // k.shape[1]) > 16 and q.dtype != F32
+    one_p = q.dtype == BF16 or (Tq * (Hq // k.shape[1]) > 16 and q.dtype != F32)
     off = np.abs(_np(g4) - want) / _bound(want, spread, size, T, d, q.dtype, got.dtype, one_p)
     assert np.isfinite(off).all() and off.max() <= 1, off.max()
     return off.max()
