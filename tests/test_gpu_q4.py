@@ -279,7 +279,7 @@ def test_lengths_of_nothing_and_beyond(dtype, G, Tq):
 
 
 @pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("G,Tq", [(2, 1), (2, 8), (4, 20), (1, 150)])
+@pytest.mark.parametrize("G,Tq", [(2, 1), (2, 8), (4, 6), (4, 12), (4, 20), (1, 150)])
 def test_what_lies_behind_the_last_token_stays_there(d, G, Tq):
     # parameters and codes of rows that nobody sees: NaN, infinities, products beyond fp16
     B, Hkv, T = 3, 2, 200
@@ -296,7 +296,7 @@ def test_what_lies_behind_the_last_token_stays_there(d, G, Tq):
 
 
 @pytest.mark.parametrize("dtype", [F16, F32])
-@pytest.mark.parametrize("G,Tq,at", [(2, 1, 70), (2, 1, 199), (2, 9, 195), (4, 30, 180), (1, 150, 60), (1, 150, 199)])
+@pytest.mark.parametrize("G,Tq,at", [(2, 1, 70), (2, 1, 199), (2, 9, 195), (4, 12, 190), (4, 30, 180), (1, 150, 60), (1, 150, 199)])
 def test_a_token_that_is_no_number_reaches_those_who_see_it(dtype, G, Tq, at):
     B, Hkv, T, d = 1, 2, 200, 128
     q = _randn(52, B, Hkv * G, Tq, d, dtype=dtype)
@@ -314,7 +314,7 @@ def test_a_token_that_is_no_number_reaches_those_who_see_it(dtype, G, Tq, at):
         assert torch.equal(got[:, :, ~sees], want[:, :, ~sees])  # to the bit: nothing else changed for them
 
 
-@pytest.mark.parametrize("G,Tq", [(4, 1), (4, 30)])
+@pytest.mark.parametrize("G,Tq", [(4, 1), (4, 5), (4, 12), (4, 30)])
 def test_scores_far_apart_and_large(G, Tq):
     # one token far above the others, at either end and in the middle; scores of thousands
     B, Hkv, T, d = 1, 1, 700, 128
@@ -370,6 +370,23 @@ def test_other_layouts_of_queries_and_outputs():
     assert torch.equal(out.transpose(1, 2), want) and torch.equal(csr.csr_q4_attn(q, *cache), want)
     _check(q, cache, want)
     _check(q[:, :, 4], cache, csr.csr_q4_attn(q[:, :, 4], *cache))   # the last token alone: 4 rows, whose probabilities are rounded otherwise
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_random_shapes(seed):
+    r = np.random.default_rng(1000 + seed)
+    d = int(r.choice([64, 128]))
+    gk, gv = (int(r.choice([g for g in (32, 64, 128) if g <= d])) for _ in range(2))
+    Hkv, G, B = int(r.integers(1, 4)), int(r.choice([1, 2, 3, 4, 7, 8])), int(r.integers(1, 4))
+    T, Tq = int(np.exp(r.uniform(0, np.log(3000)))), int(np.exp(r.uniform(0, np.log(90)))) if seed % 2 else 1
+    dtype = [F16, BF16, F32][seed % 3]
+    cache = _filled(300 + seed, B, Hkv, T, d, gk, gv)
+    q = _randn(400 + seed, B, Hkv * G, Tq, d, dtype=dtype)
+    lens, qn = r.integers(0, T + 1, B).tolist(), r.integers(0, Tq + 1, B).tolist()
+    lens[0], qn[0] = T, Tq
+    seq, ql = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in (lens, qn))
+    causal = bool(r.integers(0, 4))
+    _check(q, cache, csr.csr_q4_attn(q, *cache, seq_lens=seq, q_lens=ql, causal=causal), lens, qn, causal)
 
 
 # ---- together -----------------------------------------------------------------------------------------------------------
