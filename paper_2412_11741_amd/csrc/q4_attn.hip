@@ -278,7 +278,7 @@ __global__ __launch_bounds__(64 * W, NR == 1 && QMODE != CSR_F32 && W == 4 ? 3 :
         // Probabilities against the maxima as they are.  A lane's sum of eight tells whether one of them may have left fp16's range; the
         // maxima are moved first then, and in a wave's first turn.
         half8v ph[NR], pl[kOneP ? 1 : NR];
-        float part_sum[NR];
+        float part_sum[NR] = {};
         const auto weigh = [&](int t) __attribute__((always_inline)) {
             const float lift = kShift - top[t];
             half2v p2[4], rest[4];
@@ -308,17 +308,19 @@ __global__ __launch_bounds__(64 * W, NR == 1 && QMODE != CSR_F32 && W == 4 ? 3 :
             }
             moved = __any(largest > kMostHalf);
         }
-        if (moved) {
-            first = false;
+        if (moved) {   // only those rows' that need it: what others see changes no bit of a row
 #pragma unroll
             for (int t = 0; t < NR; ++t) {
+                int mine = first || part_sum[t] > kMostHalf;
+                mine |= __shfl_xor(mine, 16, 64);
+                mine |= __shfl_xor(mine, 32, 64);
                 float best = score[t][0];
 #pragma unroll
                 for (int j = 1; j < 8; ++j) best = fmaxf(best, score[t][j]);
                 best *= unit[t];
                 best = fmaxf(best, __shfl_xor(best, 16, 64));
                 best = fmaxf(best, __shfl_xor(best, 32, 64));
-                best = fmaxf(best, top[t]);
+                best = mine ? fmaxf(best, top[t]) : top[t];
                 const float fade = __builtin_amdgcn_exp2f(top[t] - best);
                 top[t] = best;
                 sum[t] *= fade;
@@ -326,6 +328,7 @@ __global__ __launch_bounds__(64 * W, NR == 1 && QMODE != CSR_F32 && W == 4 ? 3 :
                 for (int c = 0; c < UC; ++c) o[t][c] *= fade;
                 weigh(t);
             }
+            first = false;
         }
 #pragma unroll
         for (int t = 0; t < NR; ++t) sum[t] += part_sum[t];

@@ -210,12 +210,15 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 4 : 2) void q4_prompt_kernel(Attn
                 }
             };
             weigh();
-            if (__any(part_sum > 32.0f * 8192.0f)) {
+            if (__any(part_sum > 32.0f * 8192.0f)) {   // (only those rows': what others see changes no bit of a row)
+                int mine = part_sum > 32.0f * 8192.0f;
+                mine |= __shfl_xor(mine, 32, 64);
                 float best = c[0][0];
 #pragma unroll
                 for (int j = 1; j < 32; ++j) best = fmaxf(best, c[j >> 4][j & 15]);
                 best *= unit;
                 best = fmaxf(fmaxf(best, __shfl_xor(best, 32, 64)), top);
+                if (!mine) best = top;
                 const float fade = __builtin_amdgcn_exp2f(top - best);
                 top = best;
                 sum *= fade;

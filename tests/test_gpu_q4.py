@@ -352,6 +352,21 @@ def test_long_contexts_of_even_scores_keep_every_token():
         _check(q.to(dtype), cache, csr.csr_q4_attn(q.to(dtype), *cache))
 
 
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("B,Hq,Hkv,T,Tq", [(1, 2, 1, 700, 3), (1, 8, 2, 700, 6), (2, 8, 2, 700, 12), (1, 2, 2, 700, 150), (128, 2, 2, 300, 150)])
+def test_other_rows_change_no_bit(B, Hq, Hkv, T, Tq, dtype):
+    # one query of every sequence grows until its scores leave all others behind
+    cache = _filled(86, B, Hkv, T, 128, 64, 64)
+    q = _randn(88, B, Hq, Tq, 128, dtype=dtype)
+    want = csr.csr_q4_attn(q, *cache)
+    for size in (4.0, 64.0):
+        loud = q.clone()
+        loud[:, 0, 1] *= size
+        got = csr.csr_q4_attn(loud, *cache)
+        got[:, 0, 1] = want[:, 0, 1]
+        assert torch.equal(got, want)
+
+
 def test_the_same_call_gives_the_same_bits():
     cache = _filled(90, 2, 4, 5000, 128, 64, 64)
     q = _randn(92, 2, 8, 5, 128)
