@@ -378,8 +378,8 @@ csr_status csr_q4_read(const csr_q4_rows_desc *desc, const void *codes, const vo
  * that see no token, yield zeros.  What the cache holds behind a sequence's last token, or behind the tokens a query
  * sees, never reaches its output, NaN included.  Products of values and probabilities, scores and sums are fp32; the
  * query enters as fp16 (fp16 as it is, bf16 and fp32 times a power of two per head vector, bf16 without loss down to
- * 2^-28 of the vector's largest, fp32 as two fp16), probabilities as one fp16 (bf16 queries; fp16 queries with more than
- * 16 query rows, tokens times heads, per KV head) or as two.  The same inputs give the same bits on every run.
+ * 2^-28 of the vector's largest, fp32 as two fp16), probabilities as two fp16, or as one (bf16 queries; fp16 queries with
+ * more than 16 query rows, tokens times heads, per KV head, at some sizes).  The same inputs give the same bits on every run.
  */
 #define CSR_FLAG_NOT_CAUSAL 1u
 typedef struct {

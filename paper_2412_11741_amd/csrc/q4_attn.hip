@@ -515,40 +515,58 @@ template <int D> hipError_t run(const AttnKernelArgs &ka, int row_tiles, bool al
 
 }  // namespace
 
-// The kernel for a call's query rows, and the parts of its token axis.  Up to 64 rows per KV head the waves of a workgroup share the
-// rows, 16, 32 or 64 of them, and divide the tokens; more (and fp16 or bf16 queries) go to the kernel whose waves share the tokens
-// and divide 256 rows.  Measured, us, with the rows in fours of 16 and with 256 at their best numbers of parts: 4 x 8 (sequences
-// x KV heads) of 4096 tokens, 64 rows, 25.8 and 24.2; 16 x 8 of 8192, 36 rows, 67 and 101; 4 x 8 of 8192, 128 rows, 56 and 38; 8 of
-// 10240, 8192 rows, 447 and 330.
-//   What a call takes is close to (us, fitted to 25 shapes at up to 10 numbers of parts each)
-//     turns * (0.2 + 0.8 c) * size   turns: of 128 tokens per workgroup, c: workgroups per CU, size: of a turn; for the many rows
-//     turns * c * size               turns of 64 tokens
-//     + 3.6 in one part; in more 6.7, 0.08 for every part beyond 16 and the parts' bytes at 4 TB/s, out and in.
-// Measured at 8 pairs of 517 tokens: 8.0 us in one part, 7.8 in three, 7.0 in one of eight waves; of 8192: 56.4 in one, 13.5 in eight, 10.1 in 16, 10.6 in
-// 24; 512 pairs of 2048: 29.8 in one, 32.1 in two.
+// The kernel for a call's query rows, and the parts of its token axis.  In three kernels the waves of a workgroup share the rows, 16, 32
+// or 64 of them, and divide the tokens; in the one for many rows (fp16 and bf16 queries) they share the tokens and divide 256 rows.
+// Sharing makes codes cheaper and workgroups fewer.  What a call takes is close to (us; size: of a turn, 1, 1.36, 2.45 and 0.75 to 2.2,
+// with heads of 64 channels 0.6 of that)
+//   turns * (0.2 + 0.8 c) * size   turns: of 128 tokens per workgroup, c: workgroups per CU
+//   turns * c * size               turns of 64 tokens, for the many rows
+//   + 0, 1.5, 3, 5                 by the rows of a workgroup
+//   + 3.6 in one part; in more 6.7, 0.08 for every part beyond 16 and the parts' bytes at 4 TB/s, out and in
+// and what is least is taken, fewer rows a workgroup if 3 % less.  (70 shapes, each with all kernels and 1 to 64 parts timed: 1 % slower than
+// the fastest on the average, 20 % at most.)  Measured, us, with 16, 32, 64 and 256 rows at their best numbers of parts: 5 KV heads of 131
+// rows, 425 tokens 7.4 (eight waves), 9.8, 12.5, 13.8; 8 of 1200 rows, 300 tokens 10.6, 12.7, 15.8, 18.9; 32 of 512, 512 tokens 17.0,
+// 15.5, 17.7, 25.4; 512 of 64, 2048 tokens 99, 67, 57; 128 of 64, 700 tokens 15.6, 13.4, 20.3; 8 of 8192, 10240 tokens 625, 463, 402, 322.
+// Parts measured at 8 pairs of 517 tokens: 8.0 us in one, 7.8 in three, 7.0 in one of eight waves; of 8192: 56.4 in one, 13.5 in
+// eight, 10.1 in 16, 10.6 in 24; 512 pairs of 2048: 29.8 in one, 32.1 in two.
 void plan_q4_attn(const Q4AttnArgs &a, Q4AttnPlan *p)
 {
     const int64_t rows = (int64_t)a.G * a.Tq, blocks = (int64_t)a.B * a.Hkv;
-    const bool fp32 = a.q_dtype == CSR_F32, many = rows > 64 && !fp32;
-    p->row_tiles = many ? 2 * kPromptWaves : rows <= 16 ? 1 : rows <= 32 || fp32 ? 2 : 4;
-    const int64_t block_rows = 16 * p->row_tiles, step = many ? kPromptTile : kStep * kWaves;
-    p->row_blocks = (int32_t)((rows + block_rows - 1) / block_rows);
-    const float busy = (float)(rows < block_rows ? rows : block_rows) / block_rows;
-    const float size = (a.d == 64 ? 0.6f : 1.0f) * (many ? 0.75f + 1.45f * busy : p->row_tiles == 1 ? 1.0f : p->row_tiles == 2 ? 1.36f : 2.6f);
-    float least = INFINITY;
-    for (const int32_t splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 192, 256}) {
-        if (splits > 1 && splits > (a.T + 127) / 128) break;
-        const int64_t turns = (a.T + step * splits - 1) / (step * splits), per_cu = (blocks * p->row_blocks * splits + kCus - 1) / kCus;
-        const float join = splits == 1 ? 3.6f : 6.7f + 0.08f * (splits > 16 ? splits - 16 : 0) + (float)(blocks * rows * splits) * a.d * 8 / 4e6f;
-        const float cost = turns * (many ? (float)per_cu : 0.2f + 0.8f * per_cu) * size + join;
-        if (cost < least) {
-            least = cost;
-            p->splits = splits;
+    const uint32_t T = (uint32_t)a.T;
+    const bool fp32 = a.q_dtype == CSR_F32;
+    const int32_t most_tiles = rows <= 16 ? 1 : rows <= 32 || fp32 ? 2 : rows <= 64 ? 4 : 2 * kPromptWaves;
+    const float width = a.d == 64 ? 0.6f : 1.0f, part_bytes = (float)(blocks * rows) * (float)(a.d * 8);
+    float to_beat = INFINITY;
+    for (const int32_t tiles : {2 * kPromptWaves, 4, 2, 1}) {
+        if (tiles > most_tiles) continue;
+        const bool many = tiles > 4;
+        const int64_t block_rows = 16 * tiles, row_blocks = (rows + block_rows - 1) / block_rows, groups = many ? row_blocks * blocks : row_blocks;   // along x
+        if (tiles < most_tiles && groups > 1 << 22) break;   // (2^32 threads are the runtime's limit)
+        const uint32_t step = many ? kPromptTile : kStep * kWaves;
+        const float busy = (float)(rows < block_rows ? rows : block_rows) / (float)block_rows;
+        const float size = width * (many ? 0.75f + 1.45f * busy : tiles == 1 ? 1.0f : tiles == 2 ? 1.36f : 2.45f);
+        const float more = many ? 5.0f : tiles == 1 ? 0.0f : tiles == 2 ? 1.5f : 3.0f;
+        float least = INFINITY;
+        int32_t best = 1;
+        for (const uint32_t splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 192, 256}) {
+            if (splits > 1 && (splits > (T + 127) / 128 || groups * splits > 1 << 22)) break;
+            const float turns = (float)((T + step * splits - 1) / (step * splits)), c = (float)((blocks * row_blocks * splits + kCus - 1) / kCus);
+            const float join = splits == 1 ? 3.6f : 6.7f + 0.08f * (float)(splits > 16 ? splits - 16 : 0) + part_bytes * (float)splits / 4e6f;
+            const float cost = turns * (many ? c : 0.2f + 0.8f * c) * size + join + more;
+            if (cost < least) {
+                least = cost;
+                best = (int32_t)splits;
+            }
         }
+        // Short contexts of few pairs: eight waves, two of them to a SIMD, go through 256 tokens in 1.45 where four take 1.0 for 128.
+        const float alone = tiles == 1 && blocks * row_blocks <= kCus ? 4.25f + fmaxf(1.0f, (float)((T + 31) / 32) / kAloneWaves) * 1.45f * width : INFINITY;
+        if (fminf(least, alone) >= to_beat) continue;
+        to_beat = 0.97f * fminf(least, alone);
+        p->row_tiles = tiles;
+        p->row_blocks = (int32_t)row_blocks;
+        p->alone = alone < least;
+        p->splits = p->alone ? 1 : best;
     }
-    // Short contexts of few pairs: eight waves, two of them to a SIMD, go through 256 tokens in 1.27 where four take 1.0 for 128.
-    p->alone = p->row_tiles == 1 && blocks <= kCus && (a.T + 255) / 256 * 1.27f * size + 3.6f < least;
-    if (p->alone) p->splits = 1;
     const size_t parts = (size_t)blocks * (size_t)rows * (size_t)p->splits;
     p->off_ml = p->splits > 1 ? (parts * a.d * 4 + 255) / 256 * 256 : 0;
     p->total_bytes = p->splits > 1 ? p->off_ml + (parts * 8 + 255) / 256 * 256 : 0;

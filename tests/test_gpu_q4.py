@@ -9,6 +9,7 @@ import torch
 import paper_2412_11741_amd as csr
 from paper_2412_11741_amd import binding
 from tests import q4_reference as ref
+from tests.q4_plan import plan
 
 pytestmark = pytest.mark.gpu
 
@@ -385,6 +386,85 @@ def test_other_layouts_of_queries_and_outputs():
     assert torch.equal(out.transpose(1, 2), want) and torch.equal(csr.csr_q4_attn(q, *cache), want)
     _check(q, cache, want)
     _check(q[:, :, 4], cache, csr.csr_q4_attn(q[:, :, 4], *cache))   # the last token alone: 4 rows, whose probabilities are rounded otherwise
+
+
+# Calls of few workgroups go to the kernel of 16 rows each, whatever their rows are: those of 32, 64 and 256 need many pairs.
+MANY = [
+    # 16s of rows a workgroup, Hq, Hkv, T (twice that with heads of 64), Tq
+    (1, 8, 2, 290, 90),                     # eight waves, several workgroups along the rows
+    (2, 16, 4, 200, 7),
+    (4, 16, 4, 400, 16),
+    (4, 12, 4, 420, 19),                    # 57 rows
+    (16, 2, 2, 200, 150),
+    (16, 6, 2, 300, 99),                    # 297 rows: two workgroups, the second of 41
+]
+
+
+MANY_TYPES = [(shape, dtype) for shape in MANY for dtype in (F16, BF16, F32) if dtype != F32 or shape[0] <= 2]   # fp32 has the two smallest
+
+
+def _many(tiles, Hq, Hkv, T, Tq, d, dtype):
+    B = 2 if tiles == 1 else 128
+    (got, blocks, _, alone), _ = plan(B, Hq, Hkv, T, Tq, d, {F32: 0, F16: 1, BF16: 2}[dtype])
+    assert got == tiles and (tiles > 1 or (alone and blocks > 1))
+    return B
+
+
+@pytest.mark.parametrize("shape,dtype", MANY_TYPES)
+@pytest.mark.parametrize("d", [64, 128])
+def test_each_kernel_is_the_definitions(dtype, d, shape):
+    tiles, Hq, Hkv, T, Tq = shape
+    T *= 128 // d
+    B = _many(tiles, Hq, Hkv, T, Tq, d, dtype)
+    cache = _filled(210, B, Hkv, T, d, 32, 64)
+    q = _token_major(_randn(212, B, Hq, Tq, d, dtype=dtype))
+    r = np.random.default_rng(213)
+    lens, qn = r.integers(0, T + 1, B), r.integers(0, Tq + 1, B)
+    lens[0], qn[0], lens[1], qn[1] = T, Tq, T - 1, Tq - 1
+    seq, ql = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in (lens, qn))
+    at = sorted({0, 1, B // 2, B - 1})
+    for causal in (True, False):
+        got = csr.csr_q4_attn(q, *cache, seq_lens=seq, q_lens=ql, causal=causal)
+        _check(q[at], tuple(c[at] for c in cache), got[at], lens[at], qn[at], causal)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("shape", MANY)
+def test_each_kernel_keeps_to_the_sequences_tokens(d, shape):
+    tiles, Hq, Hkv, T, Tq = shape
+    T *= 128 // d
+    B = _many(tiles, Hq, Hkv, T, Tq, d, F16)
+    cache = _filled(220, B, Hkv, T, d, 32, 32)
+    q, seq = _randn(222, B, Hq, Tq, d), torch.arange(B, dtype=torch.int32, device="cuda") % (T - 1) + 1
+    want = csr.csr_q4_attn(q, *cache, seq_lens=seq)
+    assert torch.isfinite(want).all()
+    behind = torch.arange(T, device="cuda") >= seq[:, None]
+    for s, m in ((NAN, NAN), (float("inf"), 0.0), (60000.0, 1000.0)):
+        for k in (0, 2):
+            cache[k].masked_fill_(behind[:, None, :, None], 0xff)
+            cache[k + 1][..., 0].masked_fill_(behind[:, None, None], s)
+            cache[k + 1][..., 1].masked_fill_(behind[:, None, None], m)
+        assert torch.equal(csr.csr_q4_attn(q, *cache, seq_lens=seq), want), (s, m)
+
+
+@pytest.mark.parametrize("shape,dtype", MANY_TYPES)
+def test_each_kernel_shows_a_token_that_is_no_number(dtype, shape):
+    tiles, Hq, Hkv, T, Tq = shape
+    d, G, B = 128, Hq // Hkv, _many(*shape, 128, dtype)
+    q = _randn(232, B, Hq, Tq, d, dtype=dtype)
+    for at in (T - Tq + Tq // 2, 5):
+        sees = torch.arange(T - Tq, T, device="cuda") >= at
+        for side in (0, 2):
+            cache = _filled(230, B, Hkv, T, d, 32, 32)
+            want = csr.csr_q4_attn(q, *cache)
+            row = torch.randn(B, Hkv, 1, d, device="cuda")
+            row[:, 1, 0, 40] = NAN                               # KV head 1, second group of channels
+            csr.csr_q4_write(row, cache[side], cache[side + 1], pos0=at)
+            got = csr.csr_q4_attn(q, *cache)
+            hit = torch.zeros_like(got, dtype=torch.bool)
+            hit[:, G:2 * G, sees, 0 if side == 0 else 32:d if side == 0 else 64] = True
+            assert torch.equal(torch.isnan(got), hit)
+            assert torch.equal(got[:, :, ~sees], want[:, :, ~sees])
 
 
 @pytest.mark.parametrize("seed", range(24))
