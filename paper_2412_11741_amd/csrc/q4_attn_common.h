@@ -9,7 +9,8 @@
 namespace csr {
 namespace q4 {
 
-constexpr float kShift = 12.0f;         // p = 2^(score - maximum + kShift)
+constexpr float kShift = 12.0f;         // p = 2^(score - maximum + kShift), as two fp16
+constexpr float kShiftOne = 8.0f;       // as one
 constexpr float kMostHalf = 65504.0f;   // the largest fp16
 constexpr float kNone = -1e30f;    // a maximum before any token
 constexpr int kPromptTile = 64;    // tokens of a turn of the kernel for many rows

@@ -199,7 +199,7 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 4 : 2) void q4_prompt_kernel(Attn
             half2v p[16];
             float part_sum;
             const auto weigh = [&]() {
-                const float lift = kShift - top;
+                const float lift = kShiftOne - top;
                 part_sum = 0.0f;
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
