@@ -11,7 +11,7 @@
 // tokens of a channel a lane.  Rows are swizzled, keys by 16 bytes, values by 64, so that every read and write touches all banks.
 // Channels lie in the order their codes are converted in (0, 2, 4, 6, 1, 3, 5, 7 of a word): the queries are put in the same
 // order, the output's lanes exchange halves.
-//   8192 rows over 10240 tokens, eight KV heads (309 GFLOP): 320 to 337 us, 920 to 970 TFLOP/s, where a large library product
+//   8192 rows over 10240 tokens, eight KV heads (309 GFLOP): 320 to 350 us, 880 to 970 TFLOP/s as the clock allows, where a large library product
 // reaches 1100.  Vector and matrix instructions together, which hardly overlap between a SIMD's waves, are 89 % of its cycles
 // (counted), at the clock that the chip's power leaves; two or four waves a workgroup are slower (less sharing), the order of the
 // instructions is worth 1 %.
