@@ -18,7 +18,7 @@
 // 2^-36.  As one (bf16 queries; more than 16 rows) they keep 11, and the sum is that of the rounded ones; 2^8 times leaves more room
 // above the maximum, and 11 bits down to 2^-22 of the largest.
 //   One row of 4 x 32 x 32768 tokens (671 MB): 126 us with the join, 5.3 TB/s; 8 x 8 sequences of up to 131072 tokens, four rows
-// (944 MB): 178 us, 5.3 TB/s (a kernel that does nothing but read reaches 6.1).  Twenty rows of 16 x 8 x 8192 tokens: 35.7 us, the issue of vector
+// (944 MB): 178 us, 5.3 TB/s (a kernel that does nothing but read reaches 6.1).  Twenty rows of 16 x 8 x 8192 tokens: 36 to 38 us, the issue of vector
 // and matrix instructions, which do not overlap between a SIMD's waves here, and the join's 5.
 #include <type_traits>
 

@@ -1,10 +1,11 @@
 // Rows into and out of the 4-bit cache: quantising as they are written, reading back.
 //
 // Both move bytes: a head vector of 128 fp16 channels is 256 bytes outside and 68 to 80 in the cache.  A channel costs some
-// twenty-six vector instructions on the way in (210 a wave and eight channels, counted), three on the way out.  A thread has eight channels of one vector, 16 bytes of
-// fp16 and one word of codes; the 4 to 16 threads of a group of channels are neighbours in a row of 16 lanes, so that the
-// group's extremes come from data-parallel-primitive moves.  The threads of a wave take consecutive tokens: their codes are
-// 256 consecutive bytes.  Two or four vectors a thread, with their requests ahead, took the same time.
+// twenty-six vector instructions on the way in (210 a wave and eight channels, counted), three on the way out.  A thread has
+// eight channels of one vector, 16 bytes of fp16 and one word of codes; the 4 to 16 threads of a group of channels are
+// neighbours in a row of 16 lanes, so that the group's extremes come from data-parallel-primitive moves.  The threads of a wave
+// take consecutive tokens: their codes are 256 consecutive bytes.  Two or four vectors a thread, with their requests ahead, took
+// the same time.
 //   Written and handed back, 2 x 32 x 4096 vectors of 128 fp16: 27.4 us, 153 MB at 5.6 TB/s.  Read back to fp16, the same
 // vectors: 16.0 us, 86 MB at 5.4 TB/s; to fp32, 2 x 4 x 8 x 32768 of 64: 86.8 us, 605 MB at 7.0 TB/s (what is read lies in the
 // caches for the most part, stores go past them).
