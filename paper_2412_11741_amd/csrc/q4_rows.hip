@@ -218,15 +218,16 @@ __device__ __forceinline__ uint32_t group_params(float lo, float hi)
     return (uint32_t)s | (uint32_t)__builtin_bit_cast(uint16_t, m) << 16;
 }
 
-// The whole number next to (x - m) / s, halves to even, from one that is off by one at most: the remainder decides, which is
-// exact with what x - m lacks.
+// The whole number next to (x - m) / s, halves to even, from one that is off by one at most.  The rounded difference's distance to
+// the middle between two codes is exact where it is small (the middle is 16 bits), and compared with what the difference lacks:
+// added to it, the lacking part would be rounded away, and a value next to a middle would pass for one on it.
 __device__ __forceinline__ float decided(float x, float m, float s, float r)
 {
     const Difference t = difference(x, m);
-    const float rest = fmaf(-r, s, t.rounded) + t.rest, half = 0.5f * s;
+    const float above = fmaf(-(r + 0.5f), s, t.rounded), below = fmaf(-(r - 0.5f), s, t.rounded);
     const bool odd = ((int)r & 1) != 0;
-    if (rest > half || (rest == half && odd)) r += 1.0f;
-    else if (rest < -half || (rest == -half && odd)) r -= 1.0f;
+    if (above > -t.rest || (above == -t.rest && odd)) r += 1.0f;
+    else if (below < -t.rest || (below == -t.rest && odd)) r -= 1.0f;
     return r;
 }
 
