@@ -281,7 +281,7 @@ __global__ __launch_bounds__(64 * W, NR == 1 && QMODE != CSR_F32 && W == 4 ? 3 :
         half8v ph[NR], pl[kOneP ? 1 : NR];
         float part_sum[NR] = {};
         const auto weigh = [&](int t) __attribute__((always_inline)) {
-            const float lift = (kOneP ? kShiftOne : kShift) - top[t];
+            const float lift = fmaf(-top[t], unit[t], kOneP ? kShiftOne : kShift);
             half2v p2[4], rest[4];
             part_sum[t] = 0.0f;
 #pragma unroll
@@ -318,11 +318,10 @@ __global__ __launch_bounds__(64 * W, NR == 1 && QMODE != CSR_F32 && W == 4 ? 3 :
                 float best = score[t][0];
 #pragma unroll
                 for (int j = 1; j < 8; ++j) best = fmaxf(best, score[t][j]);
-                best *= unit[t];
                 best = fmaxf(best, __shfl_xor(best, 16, 64));
                 best = fmaxf(best, __shfl_xor(best, 32, 64));
                 best = mine ? fmaxf(best, top[t]) : top[t];
-                const float fade = __builtin_amdgcn_exp2f(top[t] - best);
+                const float fade = __builtin_amdgcn_exp2f((top[t] - best) * unit[t]);
                 top[t] = best;
                 sum[t] *= fade;
 #pragma unroll
@@ -395,7 +394,7 @@ __global__ __launch_bounds__(64 * W, NR == 1 && QMODE != CSR_F32 && W == 4 ? 3 :
         l += __shfl_xor(l, 32, 64);
         if (t > 0) __syncthreads();
         if (kg == 0) {
-            parts_top[wave][m] = top[t];
+            parts_top[wave][m] = top[t] * unit[t];
             parts_sum[wave][m] = l;
         }
 #pragma unroll
@@ -407,7 +406,7 @@ __global__ __launch_bounds__(64 * W, NR == 1 && QMODE != CSR_F32 && W == 4 ? 3 :
         for (int e = threadIdx.x; e < 16 * D / 4; e += 64 * W) {
             const int n = e / (D / 4), ch = 4 * (e % (D / 4)), r = row0 + 16 * t + n;
             if (r >= row_end) break;   // (rows ascend with e)
-            float best = kNone, all = 0.0f;
+            float best = -FLT_MAX, all = 0.0f;
             float4v value = {};
 #pragma unroll
             for (int w = 0; w < W; ++w) best = fmaxf(best, parts_top[w][n]);
@@ -444,7 +443,7 @@ __global__ __launch_bounds__(256) void q4_join_kernel(AttnKernelArgs ka)
     if (r >= ka.rows) return;
     const int side = lane / LANES, ch = 4 * (lane % LANES);
     const size_t first = (size_t)bh * ka.splits * ka.rows + r;
-    float all = 0.0f, best = kNone;
+    float all = 0.0f, best = -FLT_MAX;
     float4v value = {};
     float4v part[DEEP];
     float top[DEEP], sum[DEEP];

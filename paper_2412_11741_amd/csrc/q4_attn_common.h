@@ -12,7 +12,9 @@ namespace q4 {
 constexpr float kShift = 12.0f;         // p = 2^(score - maximum + kShift), as two fp16
 constexpr float kShiftOne = 8.0f;       // as one
 constexpr float kMostHalf = 65504.0f;   // the largest fp16
-constexpr float kNone = -1e30f;    // a maximum before any token
+// Maxima are those of the products as the matrix cores give them, before the row's unit: none is beyond 128 * 65504^2 in size, so
+// that a maximum before any token is below every one that a token may have, whatever the unit.
+constexpr float kNone = -0x1p40f;
 constexpr int kPromptTile = 64;    // tokens of a turn of the kernel for many rows
 constexpr int kPromptWaves = 8;    // of a workgroup of the kernel for many rows, 32 rows each
 
@@ -94,7 +96,9 @@ __device__ __forceinline__ RowUnit unit_of(float scale, bool shifted, float most
         u.up = most > 0.0f && most < INFINITY ? 14 - ilogbf(most) : 0;
         u.unit = ldexpf(u.unit, -u.up);
     }
-    u.unit = fminf(fmaxf(u.unit, FLT_MIN), FLT_MAX);   // (an unseen token's score, minus infinity, times 0 would be no number)
+    // An unseen token's score, minus infinity, times 0 would be no number; and kNone times the unit is one.  (Products that differ do
+    // so by 2^-48 and more: at a unit of 2^87 already nothing but the largest has a probability.)
+    u.unit = fminf(fmaxf(u.unit, FLT_MIN), 0x1p87f);
     return u;
 }
 

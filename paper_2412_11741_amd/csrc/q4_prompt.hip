@@ -199,7 +199,7 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 4 : 2) void q4_prompt_kernel(Attn
             half2v p[16];
             float part_sum;
             const auto weigh = [&]() {
-                const float lift = kShiftOne - top;
+                const float lift = fmaf(-top, unit, kShiftOne);
                 part_sum = 0.0f;
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
@@ -216,10 +216,9 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 4 : 2) void q4_prompt_kernel(Attn
                 float best = c[0][0];
 #pragma unroll
                 for (int j = 1; j < 32; ++j) best = fmaxf(best, c[j >> 4][j & 15]);
-                best *= unit;
                 best = fmaxf(fmaxf(best, __shfl_xor(best, 32, 64)), top);
                 if (!mine) best = top;
-                const float fade = __builtin_amdgcn_exp2f(top - best);
+                const float fade = __builtin_amdgcn_exp2f((top - best) * unit);
                 top = best;
                 sum *= fade;
 #pragma unroll
@@ -269,7 +268,7 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 4 : 2) void q4_prompt_kernel(Attn
             else *reinterpret_cast<float4v *>(ka.acc + to * D + ch) = v;
         }
     if (ka.splits > 1 && hh == 0 && row < row_end) {
-        ka.ml[2 * to] = top;
+        ka.ml[2 * to] = top * unit;
         ka.ml[2 * to + 1] = sum;
     }
 }

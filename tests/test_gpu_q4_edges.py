@@ -1,10 +1,12 @@
-"""The 4-bit cache on the GPU where its arithmetic is tightest: values next to the middle of two codes."""
+"""The 4-bit cache on the GPU where its arithmetic is tightest: values next to the middle of two codes, scores of any size."""
 import numpy as np
 import pytest
 import torch
 
 import paper_2412_11741_amd as csr
 from tests import q4_reference as ref
+from tests.q4_plan import plan
+from tests.test_gpu_q4 import _bound, _filled, _np, _randn
 
 pytestmark = pytest.mark.gpu
 
@@ -63,3 +65,40 @@ def test_values_a_step_of_their_type_off_a_middle(dtype):
     want_codes, want_params = ref.quantise(X.double().numpy(), group)
     codes, params = _written(X.cuda(), group)
     assert (codes == want_codes).all() and (params == want_params).all()
+
+
+# ---- attention: scores of any size --------------------------------------------------------------------------------------
+# 16s of rows a workgroup, B, Hq, Hkv, T, Tq: a call for each kernel, with one part of the token axis and with several
+KERNELS = [(1, 3, 8, 2, 517, 1), (1, 1, 8, 2, 6000, 1), (1, 2, 8, 2, 290, 90), (2, 128, 16, 4, 200, 7), (2, 1, 32, 4, 6000, 12),
+           (4, 128, 16, 4, 400, 16), (4, 16, 64, 8, 6000, 5), (16, 128, 2, 2, 200, 150), (16, 2, 64, 8, 6000, 12)]
+CALLS = [(shape, dtype) for shape in KERNELS for dtype in (F16, BF16, F32) if dtype != F32 or shape[0] <= 2]
+
+
+def _against(q, cache, got, where, scale=0.0, size=None):
+    """The output of sequences `where` against 64 bits; size: the error of a score that is granted is that of one so large (none for
+    None: products and sums that are exact)"""
+    k, v = (ref.values(cache[i][where].cpu().numpy(), cache[i + 1][where].cpu().numpy()) for i in (0, 2))
+    B, Hq, Tq, d = q[where].shape
+    T = k.shape[2]
+    want, spread, sizes = ref.attention(_np(q[where]), k, v, [T] * B, [Tq] * B, scale or d ** -0.5, True)
+    one_p = q.dtype == BF16 or (Tq * (Hq // k.shape[1]) > 16 and q.dtype != F32)
+    off = np.abs(_np(got[where]) - want) / _bound(want, spread, 0 * sizes if size is None else sizes * size, T, d, q.dtype, got.dtype, one_p)
+    assert np.isfinite(off).all() and off.max() <= 1, off.max()
+
+
+@pytest.mark.parametrize("shape,dtype", [c for c in CALLS if c[1] != F16])
+def test_rows_whose_scores_are_all_far_below_zero(shape, dtype):
+    # Every score is -2^113 / sqrt(128) = -9.2e32, or half of that from a token on: powers of two times the unit, so that products, differences
+    # and probabilities are exact.  Rows that see no token of the smaller score average the larger ones.
+    tiles, B, Hq, Hkv, T, Tq = shape
+    assert plan(B, Hq, Hkv, T, Tq, 128, {F32: 0, BF16: 2}[dtype])[0][0] == tiles
+    cache = _filled(500, B, Hkv, T, 128, 32, 64)
+    K = torch.full((B, Hkv, T, 128), 8.0, device="cuda")          # groups without spread read back as they are
+    q = torch.zeros(B, Hq, Tq, 128, dtype=dtype, device="cuda")
+    q[..., 5] = -2.0 ** 110
+    where = [0, B - 1] if T < 1000 else [0]
+    for first in (T, T - (Tq + 1) // 2, T // 3):
+        K[:, :, first:] = 4.0
+        csr.csr_q4_write(K, cache[0], cache[1])
+        got = csr.csr_q4_attn(q, *cache, out_dtype=F32)
+        _against(q, cache, got, where)
