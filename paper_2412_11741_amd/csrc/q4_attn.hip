@@ -212,7 +212,7 @@ __global__ __launch_bounds__(64 * W, NR == 1 && QMODE != CSR_F32 && W == 4 ? 3 :
 #pragma unroll
     for (int t = 0; t < NR; ++t) { top[t] = kNone; sum[t] = 0.0f; }
 
-    bool first = true;
+    bool first = true, far = false;   // far: some row's maximum
     const auto turn = [&](Raw<D> &r) __attribute__((always_inline)) {
         half8v k8[2][KM];
 #pragma unroll
@@ -277,17 +277,17 @@ __global__ __launch_bounds__(64 * W, NR == 1 && QMODE != CSR_F32 && W == 4 ? 3 :
             }
         }
         // Probabilities against the maxima as they are.  A lane's sum of eight tells whether one of them may have left fp16's range; the
-        // maxima are moved first then, and in a wave's first turn.
+        // maxima are moved first then, and in a wave's first turn, and for rows whose maximum is far from zero.
         half8v ph[NR], pl[kOneP ? 1 : NR];
         float part_sum[NR] = {};
-        const auto weigh = [&](int t) __attribute__((always_inline)) {
-            const float lift = fmaf(-top[t], unit[t], kOneP ? kShiftOne : kShift);
+        const auto weigh = [&](int t, float less) __attribute__((always_inline)) {
+            const float lift = fmaf(-(top[t] - less), unit[t], kOneP ? kShiftOne : kShift);
             half2v p2[4], rest[4];
             part_sum[t] = 0.0f;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float p0 = __builtin_amdgcn_exp2f(fmaf(score[t][2 * j], unit[t], lift));
-                const float p1 = __builtin_amdgcn_exp2f(fmaf(score[t][2 * j + 1], unit[t], lift));
+                const float p0 = __builtin_amdgcn_exp2f(fmaf(score[t][2 * j] - less, unit[t], lift));
+                const float p1 = __builtin_amdgcn_exp2f(fmaf(score[t][2 * j + 1] - less, unit[t], lift));
                 p2[j] = half2v{(_Float16)p0, (_Float16)p1};
                 if constexpr (kOneP) {
                     part_sum[t] = dot2(p2[j], part_sum[t]);
@@ -304,15 +304,16 @@ __global__ __launch_bounds__(64 * W, NR == 1 && QMODE != CSR_F32 && W == 4 ? 3 :
             float largest = 0.0f;
 #pragma unroll
             for (int t = 0; t < NR; ++t) {
-                weigh(t);
+                weigh(t, 0.0f);
                 largest = fmaxf(largest, part_sum[t]);
             }
-            moved = __any(largest > kMostHalf);
+            moved = far | (bool)__any(largest > kMostHalf);   // (no branch between the two)
         }
         if (moved) {   // only those rows' that need it: what others see changes no bit of a row
+            far = false;
 #pragma unroll
             for (int t = 0; t < NR; ++t) {
-                int mine = first || part_sum[t] > kMostHalf;
+                int mine = first || part_sum[t] > kMostHalf || is_far(top[t], unit[t]);
                 mine |= __shfl_xor(mine, 16, 64);
                 mine |= __shfl_xor(mine, 32, 64);
                 float best = score[t][0];
@@ -326,7 +327,9 @@ __global__ __launch_bounds__(64 * W, NR == 1 && QMODE != CSR_F32 && W == 4 ? 3 :
                 sum[t] *= fade;
 #pragma unroll
                 for (int c = 0; c < UC; ++c) o[t][c] *= fade;
-                weigh(t);
+                const bool apart = is_far(best, unit[t]);
+                far |= __any(apart);
+                weigh(t, apart ? best : 0.0f);
             }
             first = false;
         }

@@ -102,6 +102,11 @@ __device__ __forceinline__ RowUnit unit_of(float scale, bool shifted, float most
     return u;
 }
 
+// Probabilities are 2^(product * unit + (shift - maximum * unit)), one fused operation.  Where the maximum is far from zero the sum in
+// brackets is rounded by powers of two and more, and the largest probability would be anything from nothing to an infinity: there the
+// maximum is subtracted from the products, at every turn.  (At 2^20 a float's step is 2^-3.)
+__device__ __forceinline__ bool is_far(float top, float unit) { return fabsf(top * unit) >= 0x1p20f && top != kNone; }
+
 // The channels of a word in the order that evens() and odds() give them
 __device__ __forceinline__ constexpr int word_order(int j) { return 2 * (j & 3) + (j >> 2); }
 

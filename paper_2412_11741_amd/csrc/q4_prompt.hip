@@ -152,6 +152,7 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 4 : 2) void q4_prompt_kernel(Attn
 
     float16v o[CT] = {};
     float top = kNone, sum = 0.0f;
+    bool far = false;   // some row's maximum
     uint32_t poison = 0;   // parts of the channels that a token that is no number has reached
 
     // where a lane reads: of token n channels 16 k + 8 hh .., and for the transposing read, where lane 16 e + 4 i + f reads channels
@@ -195,23 +196,23 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 4 : 2) void q4_prompt_kernel(Attn
                     if (tb + 8 * (j >> 2) + 4 * hh + (j & 3) > limit) c[j >> 4][j & 15] = -INFINITY;
             }
             // probabilities against the maximum as it is; the sum of them as fp16 is infinite where one has left their range, and is
-            // held to 32 of 2^13: the maximum is moved first then
+            // held to 32 of 2^13: the maximum is moved first then, and for rows whose maximum is far from zero
             half2v p[16];
             float part_sum;
-            const auto weigh = [&]() {
-                const float lift = fmaf(-top, unit, kShiftOne);
+            const auto weigh = [&](float less) {
+                const float lift = fmaf(-(top - less), unit, kShiftOne);
                 part_sum = 0.0f;
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
                     const float16v &x = c[j >> 3];
                     const int e = 2 * (j & 7);
-                    p[j] = half2v{(_Float16)__builtin_amdgcn_exp2f(fmaf(x[e], unit, lift)), (_Float16)__builtin_amdgcn_exp2f(fmaf(x[e + 1], unit, lift))};
+                    p[j] = half2v{(_Float16)__builtin_amdgcn_exp2f(fmaf(x[e] - less, unit, lift)), (_Float16)__builtin_amdgcn_exp2f(fmaf(x[e + 1] - less, unit, lift))};
                     part_sum = dot2(p[j], part_sum);
                 }
             };
-            weigh();
-            if (__any(part_sum > 32.0f * 8192.0f)) {   // (only those rows': what others see changes no bit of a row)
-                int mine = part_sum > 32.0f * 8192.0f;
+            weigh(0.0f);
+            if (far | (bool)__any(part_sum > 32.0f * 8192.0f)) {   // (only those rows': what others see changes no bit of a row)
+                int mine = part_sum > 32.0f * 8192.0f || is_far(top, unit);
                 mine |= __shfl_xor(mine, 32, 64);
                 float best = c[0][0];
 #pragma unroll
@@ -223,7 +224,9 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 4 : 2) void q4_prompt_kernel(Attn
                 sum *= fade;
 #pragma unroll
                 for (int t = 0; t < CT; ++t) o[t] *= fade;
-                weigh();
+                const bool apart = is_far(top, unit);
+                far = __any(apart);
+                weigh(apart ? top : 0.0f);
             }
             sum += part_sum;
 #pragma unroll

@@ -102,3 +102,33 @@ def test_rows_whose_scores_are_all_far_below_zero(shape, dtype):
         csr.csr_q4_write(K, cache[0], cache[1])
         got = csr.csr_q4_attn(q, *cache, out_dtype=F32)
         _against(q, cache, got, where)
+
+
+@pytest.mark.parametrize("shape,dtype", CALLS)
+def test_scores_so_large_that_a_step_of_them_is_many_powers_of_two(shape, dtype):
+    # Every token has one key, from a token on half of it: the tokens with the larger score share a row's weight evenly, the others have none.
+    # Scores of 2^15 to 2^32 times log2(e), and of 2^116 (which fp16 queries do not reach), either sign; the products round.
+    tiles, B, Hq, Hkv, T, Tq = shape
+    d = 128
+    assert plan(B, Hq, Hkv, T, Tq, d, {F32: 0, F16: 1, BF16: 2}[dtype])[0][0] == tiles
+    cache = _filled(510, B, Hkv, T, d, 32, 64)
+    v = torch.from_numpy(ref.values(cache[2][:1].cpu().numpy(), cache[3][:1].cpu().numpy())).double()[0].cuda().repeat_interleave(Hq // Hkv, dim=0)
+    end = torch.arange(T - Tq + 1, T + 1, device="cuda")          # tokens that each query sees
+    before = torch.cat([torch.zeros_like(v[:, :1]), v.cumsum(1)], 1), torch.cat([torch.zeros_like(v[:, :1]), v.abs().cumsum(1)], 1)
+    mean = lambda sums, low, high: (sums[:, high] - sums[:, low]) / (high - low).clamp(min=1)[:, None]
+    key, query = _randn(511, 1, 1, 1, d, dtype=F32).abs() + 1, _randn(512, B, Hq, Tq, d, dtype=F32).abs() + 1
+    one_p = dtype == BF16 or (Tq * (Hq // Hkv) > 16 and dtype != F32)
+    for first in (T, T - (Tq + 1) // 2, T // 3):
+        for a, b in [(0, 10), (4, 10), (7, 10), (10, 10), (13, 10), (13, 13)] + [(100, 10)] * (dtype != F16):
+            K = (key * 2.0 ** b).expand(B, Hkv, T, d).clone()
+            K[:, :, first:] *= 0.5
+            csr.csr_q4_write(K, cache[0], cache[1])
+            for sign in (1.0, -1.0):
+                got = csr.csr_q4_attn((query * sign * 2.0 ** a).to(dtype), *cache, out_dtype=F32)[0].double()
+                low, high = torch.zeros_like(end), end.clamp(max=first)
+                if sign < 0:
+                    low, high = torch.where(end > first, first, 0), end
+                want, spread = mean(before[0], low, high), mean(before[1], low, high)
+                bound = _bound(want.cpu().numpy(), spread.cpu().numpy(), np.zeros(want.shape[:2]), T, d, dtype, F32, one_p)
+                off = (got - want).abs().cpu().numpy() / bound
+                assert np.isfinite(off).all() and off.max() <= 1, (first, a, b, sign, off.max())
