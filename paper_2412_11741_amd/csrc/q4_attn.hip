@@ -212,7 +212,7 @@ __global__ __launch_bounds__(64 * W, NR == 1 && QMODE != CSR_F32 && W == 4 ? 3 :
 #pragma unroll
     for (int t = 0; t < NR; ++t) { top[t] = kNone; sum[t] = 0.0f; }
 
-    bool first = true, far = false;   // far: some row's maximum
+    int look = 2;   // at the maxima whatever the sums: 2 in the first turn, 1 if a row's is far from zero (one number: two flags cost scalar registers)
     const auto turn = [&](Raw<D> &r) __attribute__((always_inline)) {
         half8v k8[2][KM];
 #pragma unroll
@@ -299,21 +299,21 @@ __global__ __launch_bounds__(64 * W, NR == 1 && QMODE != CSR_F32 && W == 4 ? 3 :
             ph[t] = join(p2[0], p2[1], p2[2], p2[3]);
             if constexpr (!kOneP) pl[t] = join(rest[0], rest[1], rest[2], rest[3]);
         };
-        bool moved = first;
-        if (!first) {
+        bool moved = true;
+        if (look < 2) {
             float largest = 0.0f;
 #pragma unroll
             for (int t = 0; t < NR; ++t) {
                 weigh(t, 0.0f);
                 largest = fmaxf(largest, part_sum[t]);
             }
-            moved = far | (bool)__any(largest > kMostHalf);   // (no branch between the two)
+            moved = (look | __any(largest > kMostHalf)) != 0;
         }
         if (moved) {   // only those rows' that need it: what others see changes no bit of a row
-            far = false;
+            int far = 0;
 #pragma unroll
             for (int t = 0; t < NR; ++t) {
-                int mine = first || part_sum[t] > kMostHalf || is_far(top[t], unit[t]);
+                int mine = look > 1 || part_sum[t] > kMostHalf || is_far(top[t], unit[t]);
                 mine |= __shfl_xor(mine, 16, 64);
                 mine |= __shfl_xor(mine, 32, 64);
                 float best = score[t][0];
@@ -328,10 +328,10 @@ __global__ __launch_bounds__(64 * W, NR == 1 && QMODE != CSR_F32 && W == 4 ? 3 :
 #pragma unroll
                 for (int c = 0; c < UC; ++c) o[t][c] *= fade;
                 const bool apart = is_far(best, unit[t]);
-                far |= __any(apart);
+                far |= __builtin_amdgcn_readfirstlane(__any(apart));
                 weigh(t, apart ? best : 0.0f);
             }
-            first = false;
+            look = far != 0;
         }
 #pragma unroll
         for (int t = 0; t < NR; ++t) sum[t] += part_sum[t];
