@@ -91,11 +91,12 @@ struct RowUnit {
 };
 __device__ __forceinline__ RowUnit unit_of(float scale, bool shifted, float most)
 {
-    RowUnit u{scale * 1.44269504088896340736f, 0};
+    RowUnit u{scale, 0};
     if (shifted) {
         u.up = most > 0.0f && most < INFINITY ? 14 - ilogbf(most) : 0;
-        u.unit = ldexpf(u.unit, -u.up);
+        u.unit = ldexpf(scale, -u.up);
     }
+    u.unit *= 1.44269504088896340736f;   // (last: a scale next to the largest float is within range by then)
     // An unseen token's score, minus infinity, times 0 would be no number; and kNone times the unit is one.  (Products that differ do
     // so by 2^-48 and more: at a unit of 2^87 already nothing but the largest has a probability.)
     u.unit = fminf(fmaxf(u.unit, FLT_MIN), 0x1p87f);

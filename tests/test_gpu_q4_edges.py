@@ -6,7 +6,7 @@ import torch
 import paper_2412_11741_amd as csr
 from tests import q4_reference as ref
 from tests.q4_plan import plan
-from tests.test_gpu_q4 import _bound, _filled, _np, _randn
+from tests.test_gpu_q4 import _bound, _check, _filled, _np, _randn
 
 pytestmark = pytest.mark.gpu
 
@@ -132,3 +132,14 @@ def test_scores_so_large_that_a_step_of_them_is_many_powers_of_two(shape, dtype)
                 bound = _bound(want.cpu().numpy(), spread.cpu().numpy(), np.zeros(want.shape[:2]), T, d, dtype, F32, one_p)
                 off = (got - want).abs().cpu().numpy() / bound
                 assert np.isfinite(off).all() and off.max() <= 1, (first, a, b, sign, off.max())
+
+
+@pytest.mark.parametrize("Tq", [1, 40])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_the_largest_scales(dtype, Tq):
+    # queries near the smallest normal float under scales up to the largest: scores of ordinary size
+    cache = _filled(520, 1, 2, 200, 128, 64, 64)
+    q = _randn(522, 1, 4, Tq, 128, dtype=F32, gain=2.0 ** -124).to(dtype)
+    for scale in (1e37, 2.3e38, 2.4e38, 3.4e38):
+        scale = float(np.float32(scale))
+        _check(q, cache, csr.csr_q4_attn(q, *cache, scale=scale, out_dtype=F32), scale=scale)
