@@ -341,7 +341,8 @@ typedef struct {
     int64_t x_stride_b, x_stride_h, x_stride_t;       /* elements between sequences, heads, tokens of X, as they
                            are (no defaults); multiples of 16 bytes, >= 0                   */
     int32_t out_dtype;  /* csr_dtype of out                                                 */
-    int64_t out_stride_b, out_stride_h, out_stride_t; /* likewise for out; >= d where there is more than one       */
+    int64_t out_stride_b, out_stride_h, out_stride_t; /* likewise for out, whose rows must not overlap: in ascending
+                           order each stride leaves room for what those below it span       */
     int64_t pos0;       /* row t of X / out is row pos0 + pos[b] + t of the cache; |pos0| <= 2^40                   */
     uint32_t flags;     /* must be 0                                                        */
 } csr_q4_rows_desc;
@@ -395,7 +396,7 @@ typedef struct {
     int32_t out_dtype;  /* csr_dtype of out                                                 */
     int64_t q_stride_b, q_stride_h, q_stride_t;       /* elements between sequences, heads, tokens of q, as they
                            are (no defaults); multiples of 16 bytes, >= 0                   */
-    int64_t out_stride_b, out_stride_h, out_stride_t; /* likewise for out; >= d where there is more than one       */
+    int64_t out_stride_b, out_stride_h, out_stride_t; /* likewise for out, whose rows must not overlap (as above)   */
     uint32_t flags;     /* CSR_FLAG_NOT_CAUSAL or 0                                         */
 } csr_q4_attn_desc;
 

@@ -1,5 +1,6 @@
 // Host side of the C ABI declared in include/csr.h: argument validation, kernel choice,
 // workspace layout.  Nothing here allocates device memory or waits for the GPU.
+#include <algorithm>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -273,7 +274,8 @@ bool valid_q4_shape(int32_t d, int32_t group)
     return (d == 64 || d == 128) && (group == 32 || group == 64 || group == 128) && group <= d;
 }
 
-// Strides of a dense operand: whole 16-byte steps, never backwards; an output's rows do not overlap
+// Strides of a dense operand: whole 16-byte steps, never backwards; an output's rows do not overlap: taken in ascending order, every stride
+// leaves room for what the ones below it span
 csr_status check_q4_strides(const char *call, const char *what, const int64_t (&stride)[3], const int64_t (&size)[3], int32_t dtype,
                             int32_t d, bool output)
 {
@@ -286,6 +288,15 @@ csr_status check_q4_strides(const char *call, const char *what, const int64_t (&
             return fail(CSR_ERR_INVALID_ARG, "%s: strides of %s must be at least d=%d (got %lld)", call, what, d, (long long)stride[k]);
         if (stride[k] > ((int64_t)1 << 48) / size[k])
             return fail(CSR_ERR_UNSUPPORTED, "%s: strides of %s are too large", call, what);
+    }
+    if (!output || size[0] == 0 || size[1] == 0 || size[2] == 0) return CSR_OK;
+    int order[3] = {0, 1, 2};
+    std::sort(order, order + 3, [&](int a, int b) { return stride[a] < stride[b]; });
+    int64_t span = d;
+    for (const int k : order) {
+        if (size[k] <= 1) continue;
+        if (stride[k] < span) return fail(CSR_ERR_INVALID_ARG, "%s: rows of %s overlap (stride %lld where %lld elements lie below it)", call, what, (long long)stride[k], (long long)span);
+        span += stride[k] * (size[k] - 1);
     }
     return CSR_OK;
 }

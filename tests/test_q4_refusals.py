@@ -1,0 +1,51 @@
+"""Calls of the 4-bit cache that would write one place twice are refused, and layouts that only look like it are not: on the host, before
+anything is launched."""
+import ctypes
+import itertools
+
+import numpy as np
+import pytest
+
+import paper_2412_11741_amd as csr
+from paper_2412_11741_amd import binding as B
+from tests.test_q4_reference import FAKE, _attn, _rows
+
+
+def _read(desc, out=FAKE):
+    """The status of csr_q4_read with an output that is misaligned: where the descriptor passes, that is what is refused"""
+    status = csr.lib().csr_q4_read(ctypes.byref(desc), FAKE, FAKE, out, None, None, None)
+    return status, csr.last_error()
+
+
+ODD = ctypes.c_void_p(0x1008)   # 8-byte aligned: refused after the descriptor has been looked at
+
+
+@pytest.mark.parametrize("b,h,t", [(1280, 128, 128), (1280, 640, 640), (640, 640, 128), (128, 1280, 248), (1272, 640, 128), (1280, 256, 384)])
+def test_outputs_whose_rows_overlap_are_refused(b, h, t):
+    status, words = _read(_rows(out_stride_b=b, out_stride_h=h, out_stride_t=t))
+    assert status == B.CSR_ERR_INVALID_ARG and "overlap" in words
+    d = _rows(out_stride_b=b, out_stride_h=h, out_stride_t=t)
+    assert csr.lib().csr_q4_write(ctypes.byref(d), FAKE, FAKE, FAKE, FAKE, None, None, None, None, None, None, None, None) == B.CSR_ERR_INVALID_ARG
+    assert "overlap" in csr.last_error()
+    a = _attn(Hq=2, Tq=5, out_stride_b=b, out_stride_h=h, out_stride_t=t)
+    assert csr.lib().csr_q4_attn_workspace_bytes(ctypes.byref(a)) == ctypes.c_size_t(-1).value and "overlap" in csr.last_error()
+
+
+@pytest.mark.parametrize("order", list(itertools.permutations(range(3))))
+@pytest.mark.parametrize("gap", [0, 8, 384])
+def test_outputs_of_any_order_and_spacing_are_taken(order, gap):
+    size, stride, span = (2, 2, 5), [0, 0, 0], 128
+    for k in order:
+        stride[k] = span + gap
+        span += stride[k] * (size[k] - 1)
+    seen = {tuple(np.dot(i, stride) + np.arange(0, 128, 8)) for i in itertools.product(*map(range, size))}
+    assert len(set(itertools.chain(*seen))) == 20 * 16            # no place twice
+    status, words = _read(_rows(out_stride_b=stride[0], out_stride_h=stride[1], out_stride_t=stride[2]), ODD)
+    assert status == B.CSR_ERR_INVALID_ARG and "aligned" in words
+    a = _attn(Hq=2, Tq=5, out_stride_b=stride[0], out_stride_h=stride[1], out_stride_t=stride[2])
+    assert csr.lib().csr_q4_attn_workspace_bytes(ctypes.byref(a)) != ctypes.c_size_t(-1).value
+
+
+def test_a_dimension_of_one_has_any_stride():
+    status, words = _read(_rows(B=1, n=1, out_stride_b=0, out_stride_h=128, out_stride_t=0), ODD)
+    assert status == B.CSR_ERR_INVALID_ARG and "aligned" in words
