@@ -359,7 +359,8 @@ size_t csr_q4_bytes(int32_t d, int32_t group);
  *   counts  [B] int32 device pointer, or NULL for n: rows of every sequence that hold a token (a padded batch)
  * Rows t >= counts[b], and rows that fall outside 0 .. T-1, are written nowhere; in out they are zeros.
  * desc2 (with X2, codes2, params2, out2) may be NULL.  It must agree with desc in B, Hkv, n, T, d, x_dtype, out_dtype and
- * pos0; group and strides are its own.  out and out2 are both given or both NULL.  No workspace.
+ * pos0; group and strides are its own.  out and out2 are both given or both NULL.  The two caches, and what the two outs write, are
+ * apart from each other and from X and X2.  No workspace.
  */
 csr_status csr_q4_write(const csr_q4_rows_desc *desc, const void *X, void *codes, void *params, void *out,
                         const csr_q4_rows_desc *desc2, const void *X2, void *codes2, void *params2, void *out2,
@@ -408,7 +409,7 @@ size_t csr_q4_attn_workspace_bytes(const csr_q4_attn_desc *desc);
  *   codesK, paramsK, codesV, paramsV                               in, the caches of keys and of values
  *   seq_lens [B] int32 device pointer, or NULL for len_b = T; larger values count as T, negative ones as 0
  *   q_lens   [B] int32 device pointer, or NULL for Tq; held to 0 .. Tq
- *   out      [B][Hq][Tq][d]  (strides as given), 16-byte aligned   out
+ *   out      [B][Hq][Tq][d]  (strides as given), 16-byte aligned   out; apart from q
  *   workspace: device memory, 256-byte aligned, >= csr_q4_attn_workspace_bytes(); may be NULL when that is 0.  Contents
  *   are undefined before and after; calls that may overlap need one each.
  */

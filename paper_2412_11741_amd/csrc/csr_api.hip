@@ -333,6 +333,26 @@ csr_status check_q4_pointers(const char *call, const void *codes, const void *pa
     return CSR_OK;
 }
 
+// Whether two arrays share a byte
+bool meet(const void *a, size_t a_bytes, const void *b, size_t b_bytes)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x < y ? y - x < a_bytes : x - y < b_bytes;
+}
+// What the two tensors of a write go to must be two caches and two outputs.  (Outputs may lie by turns in one array: only one and the
+// same is looked for.)
+csr_status check_q4_pair(const csr_q4_rows_desc &d, const csr_q4_rows_desc &d2, const void *codes, const void *params, const void *codes2,
+                         const void *params2, const void *out, const void *out2)
+{
+    const size_t rows = (size_t)d.B * (size_t)d.Hkv * (size_t)d.T, codes_bytes = rows * (size_t)d.d / 2;
+    const size_t params_bytes = rows * (size_t)(d.d / d.group) * 4, params2_bytes = rows * (size_t)(d.d / d2.group) * 4;
+    if (rows > 0 && (meet(codes, codes_bytes, codes2, codes_bytes) || meet(params, params_bytes, params2, params2_bytes) ||
+                     meet(codes, codes_bytes, params2, params2_bytes) || meet(params, params_bytes, codes2, codes_bytes)))
+        return fail(CSR_ERR_INVALID_ARG, "csr_q4_write: both tensors go to the same cache, or to caches that overlap");
+    if (out && out == out2) return fail(CSR_ERR_INVALID_ARG, "csr_q4_write: out and out2 are the same");
+    return CSR_OK;
+}
+
 csr_status check_q4_attn(const csr_q4_attn_desc *d, csr::Q4AttnArgs *args, csr::Q4AttnPlan *plan)
 {
     if (!d) return fail(CSR_ERR_INVALID_ARG, "csr_q4_attn: descriptor is NULL");
@@ -623,6 +643,7 @@ csr_status csr_q4_write(const csr_q4_rows_desc *desc, const void *X, void *codes
         return fail(CSR_ERR_INVALID_ARG, "csr_q4_write: X and out must be 16-byte aligned");
     st = check_q4_pointers("csr_q4_write", codes, params, pos, counts);
     if (st == CSR_OK) st = check_q4_pointers("csr_q4_write", codes2, params2, pos, counts);
+    if (st == CSR_OK && desc2) st = check_q4_pair(*desc, *desc2, codes, params, codes2, params2, out, out2);
     if (st != CSR_OK) return st;
     csr::Q4RowsArgs a{};
     a.side[0] = q4_side(*desc, X, codes, params, out);

@@ -143,3 +143,23 @@ def test_the_largest_scales(dtype, Tq):
     for scale in (1e37, 2.3e38, 2.4e38, 3.4e38):
         scale = float(np.float32(scale))
         _check(q, cache, csr.csr_q4_attn(q, *cache, scale=scale, out_dtype=F32), scale=scale)
+
+
+# ---- what lies side by side ---------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("d,gk,gv", [(128, 32, 128), (64, 64, 32)])
+def test_caches_and_outputs_next_to_each_other(d, gk, gv):
+    # keys' and values' codes in one array, their parameters in another, what they stand for by turns in a third
+    B, Hkv, n, T = 2, 3, 37, 41
+    K, V = _randn(530, B, Hkv, n, d), _randn(531, B, Hkv, n, d)
+    codes = torch.zeros(2, B, Hkv, T, d // 2, dtype=torch.uint8, device="cuda")
+    params = torch.zeros(B * Hkv * T * 2 * (d // gk + d // gv), dtype=F16, device="cuda")
+    cut = B * Hkv * T * 2 * (d // gk)
+    pK, pV = params[:cut].view(B, Hkv, d // gk, T, 2), params[cut:].view(B, Hkv, d // gv, T, 2)
+    out = torch.zeros(B, n, 2, Hkv, d, dtype=F16, device="cuda")
+    csr.csr_q4_write(K, codes[0], pK, V, codes[1], pV, outK=out[:, :, 0].transpose(1, 2), outV=out[:, :, 1].transpose(1, 2))
+    for k, (X, p, g) in enumerate(((K, pK, gk), (V, pV, gv))):
+        c, p1 = csr.csr_q4_alloc(B, Hkv, T, d, g)
+        want = csr.csr_q4_write(X, c, p1, values=True)
+        assert torch.equal(codes[k], c) and torch.equal(p, p1) and torch.equal(out[:, :, k].transpose(1, 2), want)
+    with pytest.raises(csr.CsrError, match="same cache"):
+        csr.csr_q4_write(K, codes[0], pK, V, codes[0], pK)

@@ -49,3 +49,23 @@ def test_outputs_of_any_order_and_spacing_are_taken(order, gap):
 def test_a_dimension_of_one_has_any_stride():
     status, words = _read(_rows(B=1, n=1, out_stride_b=0, out_stride_h=128, out_stride_t=0), ODD)
     assert status == B.CSR_ERR_INVALID_ARG and "aligned" in words
+
+
+def _write(codes, params, codes2, params2, out=None, out2=None):
+    d, d2 = _rows(), _rows()
+    p = lambda at: None if at is None else ctypes.c_void_p(at)
+    return csr.lib().csr_q4_write(ctypes.byref(d), FAKE, p(codes), p(params), p(out), ctypes.byref(d2), FAKE, p(codes2), p(params2), p(out2), None, None, None)
+
+
+CODES, PARAMS = 2 * 2 * 9 * 64, 2 * 2 * 2 * 9 * 4   # bytes of the caches of _rows()
+
+
+@pytest.mark.parametrize("at", [(0x10000, 0x20000, 0x10000, 0x30000), (0x10000, 0x20000, 0x10000 + CODES - 16, 0x30000),
+                                (0x10000, 0x20000, 0x10000 - CODES + 16, 0x30000), (0x10000, 0x20000, 0x40000, 0x20000),
+                                (0x10000, 0x20000, 0x40000, 0x20000 + PARAMS - 4), (0x10000, 0x20000, 0x20000, 0x30000), (0x10000, 0x20000, 0x40000, 0x10000)])
+def test_keys_and_values_into_one_cache_are_refused(at):
+    assert _write(*at) == B.CSR_ERR_INVALID_ARG and "same cache" in csr.last_error()
+
+
+def test_keys_and_values_into_one_output_are_refused():
+    assert _write(0x10000, 0x20000, 0x40000, 0x50000, 0x60000, 0x60000) == B.CSR_ERR_INVALID_ARG and "out2" in csr.last_error()
