@@ -187,6 +187,13 @@ def _ptr(t):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
 
 
+def _room(t):
+    """Bytes of a workspace: its elements', and none behind its memory's end (an expanded tensor has more elements than memory)"""
+    if t is None:
+        return 0
+    return max(0, min(t.numel() * t.element_size(), t.untyped_storage().nbytes() - t.storage_offset() * t.element_size()))
+
+
 def _stream():
     return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
 
@@ -286,7 +293,7 @@ def csr_encode(X, D, s, coef_dtype=None, idx_dtype=None, algo=CSR_ENCODE_AUTO, i
     need = csr_encode_workspace_bytes(desc)
     if workspace is None and need:
         workspace = torch.empty(need, dtype=torch.uint8, device=X.device)
-    wsb = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    wsb = _room(workspace)
     _check(lib().csr_encode(ctypes.byref(desc), _ptr(X), _ptr(D), _ptr(idx), _ptr(coef),
                             _ptr(workspace), wsb, _stream()))
     return idx, coef
@@ -430,8 +437,7 @@ def csr_decode_attn(q, DK, idxK, coefK, DV, idxV, coefV, scale=0.0, seq_lens=Non
     if workspace is None:
         workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
     _check(lib().csr_decode_attn(ctypes.byref(desc), _ptr(q), _ptr(DK), _ptr(idxK), _ptr(coefK), _ptr(DV),
-                                 _ptr(idxV), _ptr(coefV), _ptr(seq_lens), _ptr(out), _ptr(workspace),
-                                 workspace.numel() * workspace.element_size(), _stream()))
+                                 _ptr(idxV), _ptr(coefV), _ptr(seq_lens), _ptr(out), _ptr(workspace), _room(workspace), _stream()))
     return out
 
 
@@ -612,6 +618,5 @@ def csr_q4_attn(q, codesK, paramsK, codesV, paramsV, scale=0.0, seq_lens=None, q
         if workspace is None and need:
             workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
         _check(lib().csr_q4_attn(ctypes.byref(desc), _ptr(q), _ptr(codesK), _ptr(paramsK), _ptr(codesV), _ptr(paramsV), _ptr(seq_lens),
-                                 _ptr(q_lens), _ptr(out), _ptr(workspace),
-                                 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream()))
+                                 _ptr(q_lens), _ptr(out), _ptr(workspace), _room(workspace), _stream()))
     return out

@@ -10,6 +10,8 @@
 // which name the mistake.  Nothing has been launched in that case, except where the runtime itself reports an error.
 #include <Python.h>
 
+#include <algorithm>
+
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_cuda_dispatch.h>
@@ -97,7 +99,9 @@ struct Workspace {
     {
         if (given) {
             ptr = given->data_ptr();
-            bytes = (size_t)given->numel() * given->element_size();
+            // what its elements take, and nothing behind its memory's end: an expanded tensor has more elements than memory
+            const int64_t size = (int64_t)given->element_size(), room = (int64_t)given->storage().nbytes() - given->storage_offset() * size;
+            bytes = (size_t)std::max<int64_t>(0, std::min(given->numel() * size, room));
         } else if (need) {
             own = c10::hip::HIPCachingAllocator::get()->allocate(need);
             ptr = own.get();

@@ -163,3 +163,15 @@ def test_caches_and_outputs_next_to_each_other(d, gk, gv):
         assert torch.equal(codes[k], c) and torch.equal(p, p1) and torch.equal(out[:, :, k].transpose(1, 2), want)
     with pytest.raises(csr.CsrError, match="same cache"):
         csr.csr_q4_write(K, codes[0], pK, V, codes[0], pK)
+
+
+def test_a_workspace_of_more_elements_than_memory_is_refused():
+    cache = _filled(540, 1, 2, 6000, 128, 64, 64)
+    q = _randn(542, 1, 8, 128)
+    desc = csr.q4_attn_desc(q.unsqueeze(2), cache[0], cache[1], cache[3], torch.empty_like(q).unsqueeze(2))
+    need = csr.csr_q4_attn_workspace_bytes(desc)
+    assert need > 512
+    with pytest.raises(csr.CsrError, match="workspace"):
+        csr.csr_q4_attn(q, *cache, workspace=torch.empty(256, dtype=torch.uint8, device="cuda").expand(need, 256))
+    half = torch.empty(need // 2 * 4 + 4096, dtype=torch.uint8, device="cuda")[::2]   # every second byte: enough
+    assert torch.equal(csr.csr_q4_attn(q, *cache, workspace=half), csr.csr_q4_attn(q, *cache))

@@ -5,6 +5,7 @@ import itertools
 
 import numpy as np
 import pytest
+import torch
 
 import paper_2412_11741_amd as csr
 from paper_2412_11741_amd import binding as B
@@ -69,3 +70,10 @@ def test_keys_and_values_into_one_cache_are_refused(at):
 
 def test_keys_and_values_into_one_output_are_refused():
     assert _write(0x10000, 0x20000, 0x40000, 0x50000, 0x60000, 0x60000) == B.CSR_ERR_INVALID_ARG and "out2" in csr.last_error()
+
+
+def test_a_workspace_has_no_more_bytes_than_its_memory():
+    byte = lambda n: torch.empty(n, dtype=torch.uint8)
+    assert B._room(None) == 0 and B._room(byte(4096)) == 4096 and B._room(torch.empty(64, dtype=torch.float32)) == 256
+    assert B._room(byte(256).expand(1 << 20, 256)) == 256 and B._room(byte(4096)[256:].expand(9, 3840)) == 3840
+    assert B._room(byte(4096)[1024:2048]) == 1024 and B._room(byte(0)) == 0 and B._room(byte(4096)[::2]) == 2048
