@@ -323,7 +323,13 @@ csr_status check_q4_rows(const char *call, const csr_q4_rows_desc *d, bool reads
 
 csr::Q4RowsSide q4_side(const csr_q4_rows_desc &d, const void *x, void *codes, void *params, void *out)
 {
-    return {x, codes, params, out, {d.x_stride_b, d.x_stride_h, d.x_stride_t}, {d.out_stride_b, d.out_stride_h, d.out_stride_t}, d.group};
+    csr::Q4RowsSide s{x, codes, params, out, {}, {}, d.group};   // strides that play no part are zeros, whatever the descriptor holds
+    const int64_t size[3] = {d.B, d.Hkv, d.n}, xs[3] = {d.x_stride_b, d.x_stride_h, d.x_stride_t}, os[3] = {d.out_stride_b, d.out_stride_h, d.out_stride_t};
+    for (int k = 0; k < 3; ++k) {
+        if (x && size[k] > 1) s.x_stride[k] = xs[k];
+        if (out && size[k] > 1) s.out_stride[k] = os[k];
+    }
+    return s;
 }
 
 csr_status check_q4_pointers(const char *call, const void *codes, const void *params, const int32_t *pos, const int32_t *counts)

@@ -1,9 +1,12 @@
 """The 4-bit cache on the GPU where its arithmetic is tightest: values next to the middle of two codes, scores of any size."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
 
 import paper_2412_11741_amd as csr
+from paper_2412_11741_amd import binding
 from tests import q4_reference as ref
 from tests.q4_plan import plan
 from tests.test_gpu_q4 import _bound, _check, _filled, _np, _randn
@@ -175,3 +178,22 @@ def test_a_workspace_of_more_elements_than_memory_is_refused():
         csr.csr_q4_attn(q, *cache, workspace=torch.empty(256, dtype=torch.uint8, device="cuda").expand(need, 256))
     half = torch.empty(need // 2 * 4 + 4096, dtype=torch.uint8, device="cuda")[::2]   # every second byte: enough
     assert torch.equal(csr.csr_q4_attn(q, *cache, workspace=half), csr.csr_q4_attn(q, *cache))
+
+
+def test_strides_that_play_no_part():
+    # of X in csr_q4_read, of out in csr_q4_write without one, of dimensions of one: any numbers
+    B, Hkv, n, d, wild = 1, 2, 300, 128, (1 << 63) - 1
+    X = _randn(550, B, Hkv, n, d)
+    c, p = csr.csr_q4_alloc(B, Hkv, n, d, 64)
+    want_c, want_p = csr.csr_q4_alloc(B, Hkv, n, d, 64)
+    want = csr.csr_q4_write(X, want_c, want_p, values=True)
+    desc = binding.Q4RowsDesc(B=B, Hkv=Hkv, n=n, T=n, d=d, group=64, x_dtype=binding.CSR_F16, x_stride_b=wild, x_stride_h=n * d, x_stride_t=d,
+                              out_dtype=binding.CSR_F16, out_stride_b=wild, out_stride_h=-wild, out_stride_t=wild, pos0=0, flags=0)
+    ptr, L, stream = binding._ptr, csr.lib(), binding._stream()
+    assert L.csr_q4_write(ctypes.byref(desc), ptr(X), ptr(c), ptr(p), None, None, None, None, None, None, None, None, stream) == binding.CSR_OK
+    assert torch.equal(c, want_c) and torch.equal(p, want_p)
+    out = torch.empty_like(X)
+    desc.x_dtype, desc.x_stride_b, desc.x_stride_h, desc.x_stride_t = 77, -wild, wild, wild
+    desc.out_stride_h, desc.out_stride_t = n * d, d
+    assert L.csr_q4_read(ctypes.byref(desc), ptr(c), ptr(p), ptr(out), None, None, stream) == binding.CSR_OK
+    assert torch.equal(out, want)
