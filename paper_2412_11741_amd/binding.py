@@ -11,6 +11,7 @@ compiled part is missing or does not fit the interpreter and its PyTorch, every 
 """
 import ctypes
 import importlib.util
+import operator
 import os
 import warnings
 
@@ -508,10 +509,13 @@ def _q4_device(*tensors):
 
 
 def _q4_rows_desc(X, out, B, Hkv, n, T, d, group, pos0, dtype):
+    pos0 = operator.index(pos0)
+    if not -1 << 63 <= pos0 < 1 << 63:   # (the structure would keep its lowest 64 bits)
+        raise ValueError(f"pos0={pos0} is beyond 64 bits")
     xs, os = (t.stride() if t is not None else (0, 0, 0) for t in (X, out))
     return Q4RowsDesc(B=B, Hkv=Hkv, n=n, T=T, d=d, group=group, x_dtype=_Q4[X.dtype] if X is not None else 0,
                       x_stride_b=xs[0], x_stride_h=xs[1], x_stride_t=xs[2], out_dtype=_Q4[dtype],
-                      out_stride_b=os[0], out_stride_h=os[1], out_stride_t=os[2], pos0=int(pos0), flags=0)
+                      out_stride_b=os[0], out_stride_h=os[1], out_stride_t=os[2], pos0=pos0, flags=0)
 
 
 def csr_q4_write(K, codesK, paramsK, V=None, codesV=None, paramsV=None, pos0=0, pos=None, counts=None, values=False, outK=None, outV=None):

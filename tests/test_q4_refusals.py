@@ -77,3 +77,13 @@ def test_a_workspace_has_no_more_bytes_than_its_memory():
     assert B._room(None) == 0 and B._room(byte(4096)) == 4096 and B._room(torch.empty(64, dtype=torch.float32)) == 256
     assert B._room(byte(256).expand(1 << 20, 256)) == 256 and B._room(byte(4096)[256:].expand(9, 3840)) == 3840
     assert B._room(byte(4096)[1024:2048]) == 1024 and B._room(byte(0)) == 0 and B._room(byte(4096)[::2]) == 2048
+
+
+def test_a_first_row_that_64_bits_do_not_hold_is_refused():
+    desc = lambda pos0: B._q4_rows_desc(None, None, 1, 1, 1, 8, 64, 32, pos0, torch.float16)
+    assert desc(5).pos0 == 5 and desc(-(1 << 63)).pos0 == -(1 << 63) and desc(np.int32(7)).pos0 == 7
+    for pos0 in (1 << 63, 1 << 64, (1 << 64) + 3, -(1 << 64)):    # (the last three would be rows 0, 3 and 0)
+        with pytest.raises(ValueError, match="pos0"):
+            desc(pos0)
+    with pytest.raises(TypeError):
+        desc(2.5)
