@@ -315,8 +315,9 @@ csr_status csr_check_codes(const void *idx, int32_t idx_dtype, int64_t count, in
 /*
  * ---- A cache held in 4 bits -------------------------------------------------------------------------------------------
  * The dense alternative to the codes above: keys and values as 4-bit numbers with a scale and a minimum per group of
- * channels of every token (the group-wise integer caches that Tables 1 and 2 compare with).  Written as tokens arrive
- * (csr_q4_write), read back (csr_q4_read), attended over (csr_q4_attn).
+ * channels of every token.  (A group-wise integer cache, the kind that Tables 1 and 2 compare with, but none of theirs: those
+ * scale a key's channels over tokens.)  Written as tokens arrive (csr_q4_write), read back (csr_q4_read), attended over
+ * (csr_q4_attn).
  *
  *   codes  [B][Hkv][T][d/2]       uint8: byte j holds channel 2j in its low half, channel 2j+1 in its high half
  *   params [B][Hkv][d/group][T][2] fp16: scale s and minimum m of channels k*group .. (k+1)*group - 1 of the token
@@ -329,6 +330,7 @@ csr_status csr_check_codes(const void *idx, int32_t idx_dtype, int64_t count, in
  * value) or everywhere (a key).
  *
  * Both arrays are contiguous, codes 16-byte and params 4-byte aligned; a row no call has written holds whatever was there.
+ * Where a cache is filled by other means, m and 15 s + m are finite, or the group stands for NaN as above.
  */
 typedef struct {
     int32_t B;          /* sequences; >= 0                                                  */
@@ -378,10 +380,15 @@ csr_status csr_q4_read(const csr_q4_rows_desc *desc, const void *codes, const vo
  * qn = q_lens[b] (Tq without q_lens), query i < qn stands at token len_b - qn + i and sees the tokens up to it - its own
  * key is in the cache already.  With CSR_FLAG_NOT_CAUSAL every query sees all len_b tokens.  Queries i >= qn, and those
  * that see no token, yield zeros.  What the cache holds behind a sequence's last token, or behind the tokens a query
- * sees, never reaches its output, NaN included.  Products of values and probabilities, scores and sums are fp32; the
- * query enters as fp16 (fp16 as it is, bf16 and fp32 times a power of two per head vector, bf16 without loss down to
- * 2^-28 of the vector's largest, fp32 as two fp16), probabilities as two fp16, or as one (bf16 queries; fp16 queries with
- * more than 16 query rows, tokens times heads, per KV head, at some sizes).  The same inputs give the same bits on every run.
+ * sees, never reaches its output, NaN included.
+ * Products of values and probabilities, scores and sums are fp32.  The query enters as fp16 (fp16 as it is, bf16 and fp32
+ * times a power of two per head vector, bf16 without loss down to 2^-28 of the vector's largest, fp32 as two fp16).
+ * Probabilities enter as fp16 too, whatever out's type:
+ *   as two, 22 bits: fp32 queries; fp16 queries of up to 16 query rows (tokens times heads) per KV head
+ *   as one, 11 bits: bf16 queries
+ *   as one or two: fp16 queries of more rows - as one where a workgroup takes more than 16 of them, which is chosen by what
+ *   the call's sizes cost, T among them
+ * The same inputs give the same bits on every run.
  */
 #define CSR_FLAG_NOT_CAUSAL 1u
 typedef struct {

@@ -14,9 +14,10 @@
 //   - lane (m, kg) takes channels (d / 16) m .. of the values of tokens 8 kg .. 8 kg + 7: two tokens' words are cut into halves and
 //     joined, and every pair of codes is then one channel of two tokens.
 // Probabilities are 2^12 times their ratio to the running maximum's, which is moved when a lane's eight add up to more than an
-// fp16 holds: as two fp16 - the value and what it lacks - they keep 22 bits down to 2^-26 of the largest, and the rest to
-// 2^-36.  As one (bf16 queries; more than 16 rows) they keep 11, and the sum is that of the rounded ones; 2^8 times leaves more room
-// above the maximum, and 11 bits down to 2^-22 of the largest.
+// fp16 holds: as two fp16 - the value and what it lacks - they keep 22 bits down to 2^-14 of the largest, where what they lack meets
+// fp16's smallest step: below, steps of 2^-36 of the largest.  As one (bf16 queries; more than 16 rows a workgroup) they keep 11 bits, and
+// the sum is that of the rounded ones; 2^8 times leaves more room above the maximum, 11 bits down to 2^-22 of the largest and steps of
+// 2^-32 of it below.
 //   One row of 4 x 32 x 32768 tokens (671 MB): 126 us with the join, 5.3 TB/s; 8 x 8 sequences of up to 131072 tokens, four rows
 // (944 MB): 178 us, 5.3 TB/s (a kernel that does nothing but read reaches 6.1).  Twenty rows of 16 x 8 x 8192 tokens: 36 to 38 us, the issue of vector
 // and matrix instructions, which do not overlap between a SIMD's waves here, and the join's 5.

@@ -197,3 +197,71 @@ def test_strides_that_play_no_part():
     desc.out_stride_h, desc.out_stride_t = n * d, d
     assert L.csr_q4_read(ctypes.byref(desc), ptr(c), ptr(p), ptr(out), None, None, stream) == binding.CSR_OK
     assert torch.equal(out, want)
+
+
+# ---- probabilities: what a kernel keeps of them -------------------------------------------------------------------------
+def _kept(one_p):
+    """The part of a probability, and of the row's largest one, that its rounding may cost: one fp16 at 2^8 of the maximum (11 bits, and
+    half of fp16's smallest step), or two at 2^12"""
+    return (2.0 ** -11, 2.0 ** -33) if one_p else (2.0 ** -21, 2.0 ** -37)
+
+
+# 16s of rows a workgroup, B, Hq, Hkv, T, Tq
+TAILS = [((1, 1, 8, 2, 40000, 1), F16), ((1, 1, 8, 2, 40000, 1), BF16), ((1, 1, 8, 2, 40000, 1), F32), ((2, 16, 32, 8, 40000, 5), F16),
+         ((2, 16, 32, 8, 40000, 5), BF16), ((2, 1, 32, 4, 40000, 12), F32), ((4, 16, 64, 8, 40000, 5), F16), ((4, 16, 64, 8, 40000, 5), BF16),
+         ((16, 2, 64, 8, 40000, 12), F16), ((16, 2, 64, 8, 40000, 12), BF16)]
+
+
+@pytest.mark.parametrize("shape,dtype", TAILS)
+def test_a_long_tail_of_small_probabilities(shape, dtype):
+    # One token, whose value is zero, and 40000 others far below it that are all there is in the output: each 2^-13 of the largest probability to
+    # 2^-30.  What a kernel leaves out of them, of the products or of the sum, shows whole.
+    tiles, B, Hq, Hkv, T, Tq = shape
+    d = 128
+    assert plan(B, Hq, Hkv, T, Tq, d, {F32: 0, F16: 1, BF16: 2}[dtype])[0][0] == tiles
+    cache = csr.csr_q4_alloc(B, Hkv, T, d, 32) + csr.csr_q4_alloc(B, Hkv, T, d, 32)
+    one_p = dtype == BF16 or (dtype == F16 and tiles > 1)
+    relative, absolute = _kept(one_p)
+    end = torch.arange(T - Tq + 1, T + 1, device="cuda")
+    q = torch.zeros(B, Hq, Tq, d, dtype=dtype, device="cuda")
+    q[..., 0] = 16.0
+    for at in (0, T - Tq):                                        # the first token, and one that every query sees last but its own
+        V = _randn(560, 1, 1, T, d, dtype=F32) + 1.0
+        V[:, :, at] = 0.0
+        csr.csr_q4_write(V.expand(B, Hkv, T, d), cache[2], cache[3])
+        v = csr.csr_q4_read(cache[2][:1, :1].contiguous(), cache[3][:1, :1].contiguous(), out_dtype=F32)[0, 0].double()
+        sums, sizes = v.cumsum(0)[end - 1], v.abs().cumsum(0)[end - 1]
+        for bits in (13, 19, 23, 26, 30):
+            K = torch.zeros(1, 1, T, d, device="cuda")
+            K[:, :, at, 0] = bits * np.log(2.0) * d ** 0.5 / 16.0
+            csr.csr_q4_write(K.expand(B, Hkv, T, d), cache[0], cache[1])
+            high = float(csr.csr_q4_read(cache[0][:1, :1].contiguous(), cache[1][:1, :1].contiguous(), out_dtype=F32)[0, 0, at, 0])
+            score = high * 16.0 * d ** -0.5
+            w = np.exp(-score)                                    # of a token of the tail, for 1 of the largest
+            all_of = 1.0 + w * (end - 1).double()
+            got = csr.csr_q4_attn(q, *cache, out_dtype=F32)[0].double()
+            want = w * sums / all_of[:, None]
+            spread, total = w * sizes / all_of[:, None], sizes / all_of[:, None]
+            error = 2 * (score * (d + 4) * 2.0 ** -24 + 16 * 2.0 ** -24) + relative + (2 * (T / 32 * 8 + 64) + 8) * 2.0 ** -24
+            bound = 1.01 * (spread * error + total * absolute + want.abs() * (T * absolute)) + 1e-30
+            off = ((got - want).abs() / bound).max().item()
+            assert off <= 1, (at, bits, off)
+
+
+# B, Hq, Hkv, T, Tq, d: several workgroups along a KV head's rows, 16 each, because there are few pairs
+SIXTEENS = [(2, 8, 2, 290, 90, 128), (1, 40, 2, 300, 1, 128), (1, 4, 4, 100, 64, 64), (1, 8, 2, 700, 33, 128), (1, 2, 1, 260, 260, 128), (2, 6, 2, 400, 50, 64)]
+
+
+@pytest.mark.parametrize("shape", SIXTEENS)
+def test_sixteen_rows_a_workgroup_keep_two_fp16_of_a_probability(shape):
+    B, Hq, Hkv, T, Tq, d = shape
+    (tiles, blocks, _, _), _ = plan(B, Hq, Hkv, T, Tq, d, 1)
+    assert tiles == 1 and blocks > 1
+    cache = _filled(570, B, Hkv, T, d, 32, 32)
+    q = _randn(572, B, Hq, Tq, d)
+    got = csr.csr_q4_attn(q, *cache, out_dtype=F32)
+    k, v = (ref.values(cache[i].cpu().numpy(), cache[i + 1].cpu().numpy()) for i in (0, 2))
+    want, spread, size = ref.attention(_np(q), k, v, [T] * B, [Tq] * B, d ** -0.5, True)
+    bound = _bound(want, spread, size, T, d, F16, F32, False) + _kept(False)[1] * np.abs(v.astype(np.float64)).sum(axis=2).max()
+    off = np.abs(_np(got) - want) / bound
+    assert np.isfinite(off).all() and off.max() <= 1, off.max()
