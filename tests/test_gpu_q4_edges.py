@@ -148,6 +148,17 @@ def test_the_largest_scales(dtype, Tq):
         _check(q, cache, csr.csr_q4_attn(q, *cache, scale=scale, out_dtype=F32), scale=scale)
 
 
+@pytest.mark.parametrize("shape,dtype", CALLS)
+def test_scales_next_to_nothing(shape, dtype):
+    # scales at which the number that stands for no token yet is itself a score of ordinary size: every token weighs nearly the same
+    tiles, B, Hq, Hkv, T, Tq = shape
+    cache = _filled(525, B, Hkv, T, 128, 32, 64)
+    q = _randn(527, B, Hq, Tq, 128, dtype=dtype)
+    for scale in (1e-38, 1e-20, 1e-13, 3e-12, 5e-12, 1e-11, 1e-9) if T < 1000 else (3e-12,):
+        scale = float(np.float32(scale))
+        _against(q, cache, csr.csr_q4_attn(q, *cache, scale=scale, out_dtype=F32), [B - 1], scale=scale, size=1.0)
+
+
 # ---- what lies side by side ---------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("d,gk,gv", [(128, 32, 128), (64, 64, 32)])
 def test_caches_and_outputs_next_to_each_other(d, gk, gv):
@@ -265,3 +276,13 @@ def test_sixteen_rows_a_workgroup_keep_two_fp16_of_a_probability(shape):
     bound = _bound(want, spread, size, T, d, F16, F32, False) + _kept(False)[1] * np.abs(v.astype(np.float64)).sum(axis=2).max()
     off = np.abs(_np(got) - want) / bound
     assert np.isfinite(off).all() and off.max() <= 1, off.max()
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+def test_one_query_for_all_heads_and_tokens(dtype):
+    # queries of stride 0, along heads and along tokens
+    cache = _filled(580, 2, 2, 150, 128, 32, 64)
+    one = _randn(582, 2, 1, 1, 128, dtype=dtype)
+    for Hq, Tq in ((8, 1), (4, 9), (2, 70)):
+        q = one.expand(2, Hq, Tq, 128)
+        assert torch.equal(csr.csr_q4_attn(q, *cache), csr.csr_q4_attn(q.contiguous(), *cache))
