@@ -19,8 +19,9 @@
 // the sum is that of the rounded ones; 2^8 times leaves more room above the maximum, 11 bits down to 2^-22 of the largest and steps of
 // 2^-32 of it below.
 //   One row of 4 x 32 x 32768 tokens (671 MB): 126 us with the join, 5.3 TB/s; 8 x 8 sequences of up to 131072 tokens, four rows
-// (944 MB): 178 us, 5.3 TB/s (a kernel that does nothing but read reaches 6.1).  Twenty rows of 16 x 8 x 8192 tokens: 36 to 38 us, the issue of vector
-// and matrix instructions, which do not overlap between a SIMD's waves here, and the join's 5.
+// (944 MB): 178 us, 5.3 TB/s (a kernel that does nothing but read reaches 6.1).  Twenty rows of 16 x 8 x 8192 tokens: 35 to 38 us with the join's 5:
+// vector and matrix instructions, which do not overlap between a SIMD's waves here, are 77 % of its cycles (counted), the rest is
+// its two waves waiting.
 #include <type_traits>
 
 #include "q4_attn_common.h"
@@ -529,7 +530,9 @@ template <int D> hipError_t run(const AttnKernelArgs &ka, int row_tiles, bool al
 //   + 0, 1.5, 3, 5                 by the rows of a workgroup
 //   + 3.6 in one part; in more 6.7, 0.08 for every part beyond 16 and the parts' bytes at 4 TB/s, out and in
 // and what is least is taken, fewer rows a workgroup if 3 % less.  (70 shapes, each with all kernels and 1 to 64 parts timed: 1 % slower than
-// the fastest on the average, 20 % at most.)  Measured, us, with 16, 32, 64 and 256 rows at their best numbers of parts: 5 KV heads of 131
+// the fastest on the average, 20 % at most.)  Timed were fp16 and bf16 queries, and sequences as long as their cache; the host knows the
+// cache's rows only, and shorter ones pay for parts without tokens: one sequence of 517 tokens takes 6.9 us in 517 rows and 14.8 in 131072,
+// 64 of 2048 tokens 29.7 and 62.3.  Measured, us, with 16, 32, 64 and 256 rows at their best numbers of parts: 5 KV heads of 131
 // rows, 425 tokens 7.4 (eight waves), 9.8, 12.5, 13.8; 8 of 1200 rows, 300 tokens 10.6, 12.7, 15.8, 18.9; 32 of 512, 512 tokens 17.0,
 // 15.5, 17.7, 25.4; 512 of 64, 2048 tokens 99, 67, 57; 128 of 64, 700 tokens 15.6, 13.4, 20.3; 8 of 8192, 10240 tokens 625, 463, 402, 322.
 // Parts measured at 8 pairs of 517 tokens: 8.0 us in one, 7.8 in three, 7.0 in one of eight waves; of 8192: 56.4 in one, 13.5 in

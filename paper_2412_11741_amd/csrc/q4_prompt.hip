@@ -12,7 +12,8 @@
 // Channels lie in the order their codes are converted in (0, 2, 4, 6, 1, 3, 5, 7 of a word): the queries are put in the same
 // order, the output's lanes exchange halves.
 //   8192 rows over 10240 tokens, eight KV heads (309 GFLOP): 320 to 350 us, 880 to 970 TFLOP/s as the clock allows, where a large library product
-// reaches 1100.  Vector and matrix instructions together, which hardly overlap between a SIMD's waves, are 89 % of its cycles
+// reaches 1100 to 1320 by box (1540 with its second operand transposed); heads of 64 channels (155 GFLOP) 196 us, 790 TFLOP/s: half the
+// products to every exponential.  Vector and matrix instructions together, which hardly overlap between a SIMD's waves, are 90 % of its cycles
 // (counted), at the clock that the chip's power leaves; two or four waves a workgroup are slower (less sharing), the order of the
 // instructions is worth 1 %.
 #include <type_traits>
