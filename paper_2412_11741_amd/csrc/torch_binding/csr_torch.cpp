@@ -337,7 +337,8 @@ struct Here {
         return t && t->get_device() == device ? t : nullptr;
     }
 };
-// at::empty on the current device without the dispatcher's way there, which costs half of it (1.5 us a tensor)
+// at::empty on the current device without the dispatcher's way there, which costs half of it (1.5 us a tensor, of calls of 5): modes that
+// follow the dispatcher do not see these tensors, as they see nothing of the call that fills them
 Tensor fresh_here(at::IntArrayRef shape, ScalarType t, const Here &here)
 {
     return at::cuda::empty(shape, at::TensorOptions().dtype(t).device(at::kCUDA, (c10::DeviceIndex)here.device));
