@@ -149,6 +149,22 @@ def test_the_largest_scales(dtype, Tq):
 
 
 @pytest.mark.parametrize("shape,dtype", CALLS)
+def test_a_row_far_from_zero_changes_no_bit_of_the_others(shape, dtype):
+    # keys of 2^8, queries of 2^-8 but for one head of the last token, whose scores of 2^22 take its wave to the maxima at every turn
+    tiles, B, Hq, Hkv, T, Tq = shape
+    cache = csr.csr_q4_alloc(B, Hkv, T, 128, 64) + csr.csr_q4_alloc(B, Hkv, T, 128, 64)
+    csr.csr_q4_write(_randn(523, B, Hkv, T, 128, dtype=F32, gain=2.0 ** 8), cache[0], cache[1], _randn(524, B, Hkv, T, 128, dtype=F32), cache[2], cache[3])
+    q = _randn(528, B, Hq, Tq, 128, dtype=F32, gain=2.0 ** -8).to(dtype)
+    want = csr.csr_q4_attn(q, *cache)
+    loud = q.clone()
+    loud[:, 0, -1] *= 2.0 ** 20
+    got = csr.csr_q4_attn(loud, *cache)
+    assert torch.isfinite(got).all() and not torch.equal(got[:, 0, -1], want[:, 0, -1])
+    got[:, 0, -1] = want[:, 0, -1]
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("shape,dtype", CALLS)
 def test_scales_next_to_nothing(shape, dtype):
     # scales at which the number that stands for no token yet is itself a score of ordinary size: every token weighs nearly the same
     tiles, B, Hq, Hkv, T, Tq = shape
